@@ -312,6 +312,86 @@ int rehyat_step(const void *q_t, const void *k_win, const void *v_win,
                 int n_absorb, int stab_mode, void *stream);
 
 /*
+ * Element types of the entry points below, which take more than bf16.
+ */
+#define REHYAT_BF16 0
+#define REHYAT_FP16 1
+#define REHYAT_FP32 2
+
+/*
+ * Rotary positions of queries and keys, in front of the attention (a video
+ * block rotates every head by the frame, row and column of its token).  Pair i
+ * of the first `rot` elements of a head row is turned by the angle
+ * (position of the token on the pair's axis) * (frequency of the pair):
+ *     (a, b) -> scale * (a cos t - b sin t, b cos t + a sin t),
+ * elements rot .. d-1 are copied.  inverse = 1 turns by -t: the transpose of
+ * that map, which takes gradients of the rotated rows to gradients of the rows.
+ *
+ * Angles are formed in fixed point: a frequency is held as the 2^-64 parts of a
+ * turn that a step of one position makes (rehyat_rope_turns), so the product
+ * with a position, modulo 2^64, is the angle modulo a turn, however far the
+ * position.  cos, sin and the rotation are evaluated in fp32; results are
+ * rounded once.
+ *
+ * rehyat_rope_plan (HOST struct)
+ *   turns     DEVICE, rot / 2 values of rehyat_rope_turns
+ *   d, rot    head width (2 .. 512) and rotated part of it (even, 2 .. d)
+ *   layout    REHYAT_ROPE_INTERLEAVED: pair i is elements 2i, 2i+1;
+ *             REHYAT_ROPE_HALF: elements i, i + rot/2
+ *   axes      1 .. 3; section[x] pairs in a row belong to axis x (each >= 1, they
+ *             add up to rot / 2; the rest of `section` is not read)
+ *   scale     factor on rotated elements (1, or that of a method which scales
+ *             frequencies for long contexts)
+ * rehyat_rope_positions (HOST struct)
+ *   data      NULL: token n of every sequence stands at (start + n), at
+ *             (start + n / cols, n % cols) or at (start + n / (rows cols),
+ *             n / cols % rows, n % cols), by the number of axes.
+ *             Otherwise DEVICE integers of `bits` (32 or 64): position x of token
+ *             n of sequence b at data[b stride_b + n stride_n + x]
+ *             (stride_b 0: the same for all); negative ones are allowed.
+ * rehyat_rope_operand (HOST struct): a tensor of `heads` rows of d elements for
+ *   each of B x N tokens.  Strides in elements (>= 0; those of x may be 0), rows
+ *   themselves contiguous, pointers aligned to an element: token-major projections
+ *   can be read and head-major attention operands, or rows of a K window, written.
+ *   out is x itself (same strides) or does not overlap it; rows of out do not
+ *   overlap each other.
+ *
+ * One or two operands (queries; keys, whose number of heads may differ) of one
+ * `type` (REHYAT_BF16 / FP16 / FP32) are turned in one launch.  N may be 1 (one
+ * new token for each of B sequences, their positions in device memory).
+ * Supported: B * N < 2^31 / d (rounded down), heads <= 65535.
+ * No workspace, no library state.  Errors: REHYAT_E_NULL, REHYAT_E_SHAPE.
+ */
+#define REHYAT_ROPE_INTERLEAVED 0
+#define REHYAT_ROPE_HALF 1
+typedef struct {
+  const uint64_t *turns;
+  int32_t d, rot, layout, axes;
+  int32_t section[3];
+  float scale;
+} rehyat_rope_plan;
+typedef struct {
+  const void *data;
+  int64_t stride_b, stride_n;
+  int64_t start;
+  int32_t bits;
+  int32_t rows, cols;
+} rehyat_rope_positions;
+typedef struct {
+  const void *x;
+  void *out;
+  int64_t x_stride_b, x_stride_h, x_stride_n;
+  int64_t out_stride_b, out_stride_h, out_stride_n;
+  int32_t heads;
+} rehyat_rope_operand;
+/* HOST: radians a position (any finite value) -> 2^-64 parts of a turn. */
+int rehyat_rope_turns(const double *radians, int n, uint64_t *turns);
+int rehyat_rope(const rehyat_rope_operand *operands, int n_operands,
+                const rehyat_rope_plan *plan,
+                const rehyat_rope_positions *positions, int B, int N, int type,
+                int inverse, void *stream);
+
+/*
  * Running state of the chunk-wise RNN (Eq. 14-15, 17-18) after absorbing
  * tokens [0, upto) of every head, as the state kernels compute it:
  *   S_out [B, H, dprime, d] fp32,  z_out [B, H, dprime] fp32  (DEVICE)

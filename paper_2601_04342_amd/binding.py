@@ -6,6 +6,7 @@ if the library is missing or cannot be loaded, importing a symbol from it
 raises.
 """
 import ctypes
+import math
 import os
 
 import torch
@@ -22,6 +23,7 @@ EXPORTS = ("rehyat_chunk_plan", "rehyat_workspace_bytes", "rehyat_set_workspace"
            "rehyat_forward", "rehyat_forward_ex", "rehyat_forward_ws", "rehyat_forward_noalloc",
            "rehyat_step", "rehyat_state", "rehyat_shutdown",
            "rehyat_phi_backward", "rehyat_phi_backward_workspace_bytes",
+           "rehyat_rope", "rehyat_rope_turns",
            "rehyat_status_string", "rehyat_version", "rehyat_last_hip_error",
            "rehyat_attn_kernel_name",
            "rehyat_profile_enable", "rehyat_profile_read", "rehyat_debug_set_xcd_mask")
@@ -48,6 +50,25 @@ class ForwardSaved(ctypes.Structure):
 
 
 BACKWARD_MAX_CHUNKS = 1024
+_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
+
+
+class RopePlan(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("d", ctypes.c_int32), ("rot", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("axes", ctypes.c_int32), ("section", ctypes.c_int32 * 3),
+                ("scale", ctypes.c_float)]
+
+
+class RopePositions(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_n", ctypes.c_int64),
+                ("start", ctypes.c_int64), ("bits", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("cols", ctypes.c_int32)]
+
+
+class RopeOperand(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p)] + [
+        (f"{t}_stride_{n}", ctypes.c_int64) for t in ("x", "out") for n in "bhn"] + [("heads", ctypes.c_int32)]
 
 
 class RehyatError(RuntimeError):
@@ -105,6 +126,11 @@ def _load():
     lib.rehyat_phi_backward.argtypes = [vp, vp, vp, ctypes.POINTER(PhiParams), vp, vp,
                                         ctypes.POINTER(ForwardSaved), ctypes.POINTER(PhiGrads),
                                         ci, ci, ci, ci, ci, ci, ci, vp, ctypes.c_size_t, vp]
+    lib.rehyat_rope_turns.restype = ci
+    lib.rehyat_rope_turns.argtypes = [ctypes.POINTER(ctypes.c_double), ci, ctypes.POINTER(ctypes.c_uint64)]
+    lib.rehyat_rope.restype = ci
+    lib.rehyat_rope.argtypes = [ctypes.POINTER(RopeOperand), ci, ctypes.POINTER(RopePlan),
+                                ctypes.POINTER(RopePositions), ci, ci, ci, ci, vp]
     lib.rehyat_shutdown.restype = ci
     lib.rehyat_shutdown.argtypes = []
     lib.rehyat_status_string.restype = ctypes.c_char_p
@@ -417,3 +443,157 @@ def phi_backward(q, k, v, phi, grad_out, T, HW, chunk, overlap=0, workspace=None
     if rc != OK:
         raise RehyatError(rc, "rehyat_phi_backward")
     return grads, out
+
+
+def _elsewhere(t, stream):
+    """What to enter so that work on ``t`` and what is allocated for it belong to ``stream`` (None: the current
+    stream of the tensor's device); None where that is so already."""
+    if stream is not None:
+        if stream.device != t.device:
+            raise ValueError("the stream belongs to another device than the tensors")
+        return torch.cuda.stream(stream)
+    here = _current_device() if _current_device is not None else torch.cuda.current_device()
+    return torch.cuda.device(t.device) if here != t.get_device() else None
+
+
+class Rope:
+    """Rotary positions of heads of width ``d``, of which the first ``rot`` elements turn.
+
+    ``layout``: "interleaved" (pairs 2i, 2i+1) or "half" (pairs i, i + rot/2).  ``sections``: pairs of each axis
+    (default: one axis); pair i of an axis with n pairs turns by base^(-i/n) radians a position.  ``scaling`` for
+    contexts longer than the ones trained on, of the first axis: dict(kind=..., factor=s) with kind "linear" (positions
+    divided by s), "base" (base times s^(n/(n-1)): the slowest pair is divided by s, the fastest kept) or "parts" (with
+    original=L: pairs that make fewer than ``low`` = 1 turns in L positions are divided by s, those of more than
+    ``high`` = 32 are kept, a ramp between them; rotated values times 0.1 ln s + 1).  ``freqs`` (radians a position,
+    one for each pair) and ``scale`` replace all that."""
+
+    def __init__(self, d, rot=None, layout="interleaved", base=10000.0, sections=None, scaling=None, freqs=None,
+                 scale=None, device="cuda"):
+        rot = d if rot is None else rot
+        if not 2 <= rot <= d <= 512 or rot % 2:
+            raise ValueError("rot must be even, 2 <= rot <= d <= 512")
+        sections = (rot // 2,) if sections is None else tuple(int(n) for n in sections)
+        if not 1 <= len(sections) <= 3 or min(sections) < 1 or sum(sections) != rot // 2:
+            raise ValueError("sections must be one to three positive counts of pairs that add up to rot / 2")
+        if layout not in ROPE_LAYOUTS:
+            raise ValueError(f"layout must be one of {tuple(ROPE_LAYOUTS)}")
+        mu = 1.0
+        if freqs is None:
+            freqs = []
+            for axis, n in enumerate(sections):
+                f, m = self._frequencies(n, float(base), scaling if axis == 0 else None)
+                freqs.append(f)
+                mu *= m
+            freqs = torch.cat(freqs)
+        elif scaling is not None:
+            raise ValueError("give either freqs or scaling")
+        freqs = torch.as_tensor(freqs, dtype=torch.float64).detach().cpu().contiguous()
+        if freqs.shape != (rot // 2,):
+            raise ValueError("freqs must hold rot / 2 values")
+        self.d, self.rot, self.layout, self.sections = d, rot, layout, sections
+        self.freqs, self.scale = freqs, mu if scale is None else float(scale)
+        turns = torch.empty(rot // 2, dtype=torch.int64)
+        rc = _load().rehyat_rope_turns(ctypes.cast(freqs.data_ptr(), ctypes.POINTER(ctypes.c_double)), rot // 2,
+                                       ctypes.cast(turns.data_ptr(), ctypes.POINTER(ctypes.c_uint64)))
+        if rc != OK:
+            raise RehyatError(rc, "rehyat_rope_turns")
+        self.turns = turns.to(device)
+        self._plan = RopePlan(self.turns.data_ptr(), d, rot, ROPE_LAYOUTS[layout], len(sections),
+                              (ctypes.c_int32 * 3)(*sections), self.scale)
+
+    @staticmethod
+    def _frequencies(n, base, scaling):
+        """n frequencies of one axis in 64 bits, and the factor on rotated values."""
+        if scaling is None:
+            return base ** (-torch.arange(n, dtype=torch.float64) / n), 1.0
+        kind, s = scaling["kind"], float(scaling["factor"])
+        if kind not in ("linear", "base", "parts") or not s > 0:
+            raise ValueError('scaling needs kind "linear", "base" or "parts" and a positive factor')
+        if kind == "base" and n > 1:
+            base *= s ** (n / (n - 1))
+        f = base ** (-torch.arange(n, dtype=torch.float64) / n)
+        if kind == "linear":
+            return f / s, 1.0
+        if kind == "base":
+            return f, 1.0
+        low, high = float(scaling.get("low", 1.0)), float(scaling.get("high", 32.0))
+        if not low < high:
+            raise ValueError("scaling by parts needs low < high")
+        made = float(scaling["original"]) * f / (2 * math.pi)
+        keep = ((made - low) / (high - low)).clamp(0.0, 1.0)
+        return f * keep + f / s * (1.0 - keep), 0.1 * math.log(s) + 1.0 if s > 1 else 1.0
+
+    @classmethod
+    def video(cls, d, layout="interleaved", base=10000.0, scaling=None, device="cuda"):
+        """Heads that turn by frame, row and column: a third of the pairs each, the frame takes what is left over."""
+        third = d // 2 // 3
+        return cls(d, layout=layout, base=base, sections=(d // 2 - 2 * third, third, third), scaling=scaling,
+                   device=device)
+
+
+def _rope_operand(x, out, plan, like):
+    if x.dim() != 4 or x.dtype not in _TYPES or not x.is_cuda or x.stride(3) != 1:
+        raise TypeError("q and k must be CUDA tensors [B, H, N, d] in bf16, fp16 or fp32 with contiguous rows")
+    B, H, N, d = x.shape
+    if d != plan.d or (like is not None and (like.shape[0], like.shape[2]) != (B, N)):
+        raise ValueError("q and k must have the plan's head width, and one number of sequences and tokens")
+    if like is not None and (like.dtype != x.dtype or like.device != x.device):
+        raise TypeError("q and k must be of one type and on one device")
+    if out is None:
+        out = torch.empty((B, H, N, d), device=x.device, dtype=x.dtype)
+    elif out.shape != x.shape or out.dtype != x.dtype or out.device != x.device or out.stride(3) != 1:
+        raise TypeError("out must match its operand, with contiguous rows")
+    (xb, xh, xn, _), (ob, oh, on, _) = x.stride(), out.stride()
+    return RopeOperand(x.data_ptr(), out.data_ptr(), xb, xh, xn, ob, oh, on, H), out
+
+
+def rope(q, k, plan, grid=None, start=0, positions=None, inverse=False, out=None, stream=None):
+    """Queries and keys turned by their positions in one launch.  q, k: CUDA bf16 / fp16 / fp32 [B, H, N, d] with any
+    strides but contiguous rows (token-major projections as x.view(B, N, H, d).transpose(1, 2)); k may be None or have
+    another number of heads.  ``plan``: a ``Rope``.
+
+    Positions: ``positions``, CUDA int32 or int64 [N] or [B, N] ([N, axes], [B, N, axes] for more than one axis), or the
+    place in a grid: with axes = 3 and grid=(rows, cols) token n stands at frame start + n // (rows cols), row
+    n // cols % rows, column n % cols; with two axes and grid=(cols,) at (start + n // cols, n % cols); with one at
+    start + n.  ``inverse=True`` turns back, which is also the gradient.  ``out``: tensors to write, of any strides (a
+    part of a K window), or the operands themselves; new contiguous ones by default.  Returns (q', k'), or q' without k."""
+    ctx = _elsewhere(q, stream) if q.is_cuda else None
+    if ctx is not None:
+        with ctx:
+            return rope(q, k, plan, grid, start, positions, inverse, out)
+    lib = _load()
+    outs = (None, None) if out is None else (out if isinstance(out, (tuple, list)) else (out, None))
+    ops = (RopeOperand * 2)()
+    ops[0], q_out = _rope_operand(q, outs[0], plan, None)
+    k_out = None
+    if k is not None:
+        ops[1], k_out = _rope_operand(k, outs[1], plan, q)
+    if plan.turns.device != q.device:
+        raise ValueError("the plan is on another device than the tensors")
+    B, _, N, _ = q.shape
+    axes = len(plan.sections)
+    pos = RopePositions(start=int(start))
+    if positions is not None:
+        if grid is not None or start != 0:
+            raise ValueError("give either positions or a grid and a start")
+        tail = () if axes == 1 else (axes,)
+        if positions.dtype not in (torch.int32, torch.int64) or positions.device != q.device:
+            raise TypeError("positions must be int32 or int64 on the tensors' device")
+        if tuple(positions.shape) not in ((N,) + tail, (B, N) + tail) or (tail and positions.stride(-1) != 1):
+            raise ValueError(f"positions must have shape {(N,) + tail} or {(B, N) + tail}")
+        strides = positions.stride()[:positions.dim() - len(tail)]
+        pos.data, pos.bits = positions.data_ptr(), 32 if positions.dtype == torch.int32 else 64
+        pos.stride_b, pos.stride_n = strides if len(strides) == 2 else (0, strides[0])
+    elif axes > 1:
+        if grid is None or len(grid) != axes - 1:
+            raise ValueError(f"a plan of {axes} axes needs a grid of {axes - 1} sizes, or positions")
+        if not all(1 <= int(n) < 2**31 for n in grid):
+            raise ValueError("the sizes of a grid must be positive and fit 32 bits")
+        pos.rows, pos.cols = (0, int(grid[0])) if axes == 2 else (int(grid[0]), int(grid[1]))
+    elif grid is not None:
+        raise ValueError("a plan of one axis takes no grid")
+    rc = lib.rehyat_rope(ops, 1 if k is None else 2, ctypes.byref(plan._plan), ctypes.byref(pos), B, N,
+                         _TYPES[q.dtype], int(bool(inverse)), _stream_handle(None))
+    if rc != OK:
+        raise RehyatError(rc, "rehyat_rope")
+    return q_out if k is None else (q_out, k_out)

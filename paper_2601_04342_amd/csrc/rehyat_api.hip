@@ -11,6 +11,7 @@
 #include <mutex>
 
 #include "../../include/rehyat.h"
+#include "rehyat_host.h"
 #include "rehyat_kernels.h"
 
 namespace {
@@ -54,11 +55,6 @@ struct SideStream {
 };
 SideStream g_side[kMaxDevices];
 
-int hip_fail(hipError_t e, const char* what) {
-  snprintf(g_hip_err, sizeof(g_hip_err), "%s: %s", what, hipGetErrorString(e));
-  return REHYAT_E_HIP;
-}
-
 // optional per-kernel timing with HIP events on the caller's stream (calls that use the
 // library-held workspace only: those are serialised by g_mu)
 constexpr int kProfKinds = 3;  // state, prefix, attention
@@ -90,8 +86,6 @@ struct ProfScope {
     if (slot >= 0) (void)hipEventRecord(g_prof.end[slot], st);
   }
 };
-
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct WsLayout {
   size_t partial, state_s, state_z, carry, total;
@@ -177,9 +171,6 @@ int ensure_workspace(size_t need, hipStream_t st, char** base) {
   *base = (char*)p;
   return REHYAT_OK;
 }
-
-bool aligned16(const void* p) { return (((uintptr_t)p) & 15) == 0; }
-bool aligned4(const void* p) { return (((uintptr_t)p) & 3) == 0; }
 
 int check_phi(const rehyat_phi_params* p, int d) {
   if (!p) return REHYAT_E_NULL;
@@ -755,6 +746,11 @@ Slots slots_that_fit(int B, int H, int d, int dp, size_t bytes) {
 }
 
 }  // namespace
+
+int rehyat::hip_fail(hipError_t e, const char* what) {
+  snprintf(g_hip_err, sizeof(g_hip_err), "%s: %s", what, hipGetErrorString(e));
+  return REHYAT_E_HIP;
+}
 
 extern "C" {
 

@@ -1,0 +1,22 @@
+// What the host layers of the library share.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/rehyat.h"
+
+namespace rehyat {
+
+// keeps the error's text for rehyat_last_hip_error; returns REHYAT_E_HIP
+int hip_fail(hipError_t e, const char* what);
+
+inline bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+inline bool aligned16(const void* p) { return aligned(p, 16); }
+inline bool aligned4(const void* p) { return aligned(p, 4); }
+inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+inline bool valid_type(int t) { return t == REHYAT_BF16 || t == REHYAT_FP16 || t == REHYAT_FP32; }
+inline size_t type_bytes(int t) { return t == REHYAT_FP32 ? 4 : 2; }
+
+}  // namespace rehyat

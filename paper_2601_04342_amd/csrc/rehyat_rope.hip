@@ -1,0 +1,220 @@
+// Rotary positions of queries and keys for gfx950: kernel and host layer of rehyat_rope.
+//
+// Pair i of a head row turns by angle = position * frequency.  Frequencies come as 2^-64 parts of a turn a position, so
+// the 64-bit product, which wraps, IS the angle modulo a turn; its upper 32 bits (2^-32 of a turn is 1.5e-9 rad) give the
+// quadrant and an angle within an eighth of a turn, where short series for cos and sin serve.  No far position loses more
+// than a near one.
+//
+// Bound by HBM: each element is read and written once, and needs 3 flops.  A thread keeps the cos and sin of its pairs
+// and walks over the heads of its token with them, since they are the same for every head.
+#include <cmath>
+
+#include "rehyat_elem.h"
+#include "rehyat_host.h"
+
+namespace rehyat {
+namespace {
+
+struct RopeOperand {
+  const void* x;
+  void* out;
+  int64_t xb, xh, xn, ob, oh, on;
+  int heads;
+};
+
+struct RopeArgs {
+  RopeOperand op[2];
+  int groups0;                   // blockIdx.y below it: heads of op[0], from it on: of op[1]
+  int group;                     // heads of a group
+  const uint64_t* turns;
+  const void* pos;               // explicit positions, or null
+  int64_t pos_b, pos_n;
+  uint64_t start;
+  int pos_bits;
+  uint32_t items, slots;         // B * N * slots; pieces of a row
+  uint32_t N, frame, cols;       // frame: tokens of one step of the first axis
+  int rot, axes, sec1, sec2;     // pairs from sec1 on belong to axis 1, from sec2 on to axis 2
+  uint32_t copies_from;          // slots from here on copy
+  float scale, sign;
+};
+
+// cos and sin of an angle given in 2^-32 turns: within an eighth of a turn of the nearest quarter, the series in the
+// angle (the first term left out is below 2e-9 of the result), then the quarter turns.
+__device__ __forceinline__ void cos_sin(uint32_t t, float* c, float* s) {
+  const uint32_t quarter = (t + 0x20000000u) >> 30;
+  const float x = (float)(int32_t)(t - (quarter << 30)) * 1.46291807926715968e-9f;   // 2 pi 2^-32
+  const float y = x * x;
+  const float sn = x + x * y * (-1.f / 6 + y * (1.f / 120 + y * (-1.f / 5040 + y * (1.f / 362880))));
+  const float cs = 1.f + y * (-0.5f + y * (1.f / 24 + y * (-1.f / 720 + y * (1.f / 40320 + y * (-1.f / 3628800)))));
+  const float a = quarter & 1 ? sn : cs, b = quarter & 1 ? cs : sn;
+  *c = quarter == 1 || quarter == 2 ? -a : a;
+  *s = quarter >= 2 ? -b : b;
+}
+
+template <typename E, int LAYOUT>
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+  typedef typename E::store T;
+  const uint32_t i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= a.items) return;
+  const uint32_t token = i / a.slots, slot = i - token * a.slots;
+  const uint32_t b = token / a.N, n = token - b * a.N;
+  const bool second = (int)blockIdx.y >= a.groups0;
+  const RopeOperand& op = second ? a.op[1] : a.op[0];
+  const int h0 = ((int)blockIdx.y - (second ? a.groups0 : 0)) * a.group;
+  const int h1 = h0 + a.group < op.heads ? h0 + a.group : op.heads;
+  const T* x = (const T*)op.x + b * op.xb + n * op.xn + h0 * op.xh;
+  T* out = (T*)op.out + b * op.ob + n * op.on + h0 * op.oh;
+
+  if (slot >= a.copies_from) {
+    const uint32_t col = a.rot + slot - a.copies_from;
+    for (int h = h0; h < h1; ++h, x += op.xh, out += op.oh) out[col] = x[col];
+    return;
+  }
+  const int pair = slot, axis = pair >= a.sec2 ? 2 : pair >= a.sec1 ? 1 : 0;
+  uint64_t pos;   // modulo 2^64
+  if (a.pos) {
+    const int64_t at = b * a.pos_b + n * a.pos_n + axis;
+    pos = a.pos_bits == 64 ? ((const int64_t*)a.pos)[at] : (int64_t)((const int32_t*)a.pos)[at];
+  } else {
+    const uint32_t f = n / a.frame, r = n - f * a.frame;
+    pos = axis == 0 ? a.start + f : axis == a.axes - 1 ? r % a.cols : r / a.cols;
+  }
+  float c, s;
+  cos_sin((uint32_t)((pos * a.turns[pair]) >> 32), &c, &s);
+  c *= a.scale;
+  s *= a.scale * a.sign;
+  const uint32_t first = LAYOUT == REHYAT_ROPE_INTERLEAVED ? 2 * slot : slot;
+  const uint32_t other = LAYOUT == REHYAT_ROPE_INTERLEAVED ? first + 1 : first + a.rot / 2;
+  for (int h = h0; h < h1; ++h, x += op.xh, out += op.oh) {
+    const float u = E::get(x[first]), v = E::get(x[other]);
+    out[first] = E::put(u * c - v * s);
+    out[other] = E::put(v * c + u * s);
+  }
+}
+
+template <typename E>
+void launch(const RopeArgs& a, int layout, dim3 grid, hipStream_t st) {
+  if (layout == REHYAT_ROPE_INTERLEAVED)
+    rope_kernel<E, REHYAT_ROPE_INTERLEAVED><<<grid, 256, 0, st>>>(a);
+  else
+    rope_kernel<E, REHYAT_ROPE_HALF><<<grid, 256, 0, st>>>(a);
+}
+
+// Whether the rows of an output with these strides are apart: every dimension steps over all that the smaller ones span.
+bool rows_apart(int64_t d, int64_t sb, int64_t sh, int64_t sn, int64_t B, int64_t H, int64_t N) {
+  int64_t stride[3] = {sb, sh, sn}, extent[3] = {B, H, N};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2 - i; ++j)
+      if (stride[j] > stride[j + 1]) {
+        int64_t t = stride[j];
+        stride[j] = stride[j + 1], stride[j + 1] = t;
+        t = extent[j], extent[j] = extent[j + 1], extent[j + 1] = t;
+      }
+  int64_t span = d;
+  for (int i = 0; i < 3; ++i) {
+    if (extent[i] == 1) continue;
+    if (stride[i] < span) return false;
+    span += stride[i] * (extent[i] - 1);
+  }
+  return true;
+}
+
+}  // namespace
+}  // namespace rehyat
+
+using namespace rehyat;
+
+extern "C" {
+
+int rehyat_rope_turns(const double* radians, int n, uint64_t* turns) {
+  if (!radians || !turns) return REHYAT_E_NULL;
+  if (n < 1) return REHYAT_E_SHAPE;
+  for (int i = 0; i < n; ++i)
+    if (!std::isfinite(radians[i])) return REHYAT_E_SHAPE;
+  for (int i = 0; i < n; ++i) {
+    long double t = (long double)radians[i] / 6.28318530717958647692528676655900577L;
+    t -= std::floor(t);                       // in [0, 1]: 1 where a tiny negative one rounds up
+    t = std::ldexp(t, 64);
+    turns[i] = t >= 18446744073709551615.0L ? 0 : (uint64_t)t;
+  }
+  return REHYAT_OK;
+}
+
+int rehyat_rope(const rehyat_rope_operand* operands, int n_operands, const rehyat_rope_plan* plan,
+                const rehyat_rope_positions* positions, int B, int N, int type, int inverse, void* stream) {
+  if (!operands || !plan || !positions || !plan->turns) return REHYAT_E_NULL;
+  if (n_operands < 1 || n_operands > 2 || B < 1 || N < 1 || !valid_type(type)) return REHYAT_E_SHAPE;
+  if (inverse != 0 && inverse != 1) return REHYAT_E_SHAPE;
+  const int d = plan->d, rot = plan->rot, axes = plan->axes;
+  if (d < 2 || d > 512 || rot < 2 || rot > d || rot % 2) return REHYAT_E_SHAPE;
+  if (plan->layout != REHYAT_ROPE_INTERLEAVED && plan->layout != REHYAT_ROPE_HALF) return REHYAT_E_SHAPE;
+  if (axes < 1 || axes > 3 || !std::isfinite(plan->scale)) return REHYAT_E_SHAPE;
+  int64_t pairs = 0;
+  for (int x = 0; x < axes; ++x) {
+    if (plan->section[x] < 1) return REHYAT_E_SHAPE;
+    pairs += plan->section[x];
+  }
+  if (pairs != rot / 2) return REHYAT_E_SHAPE;
+  if (!aligned(plan->turns, 8)) return REHYAT_E_SHAPE;
+  if ((int64_t)B * N >= ((int64_t)1 << 31) / d) return REHYAT_E_SHAPE;
+  const size_t es = type_bytes(type);
+
+  RopeArgs a{};
+  if (positions->data) {
+    if (positions->bits != 32 && positions->bits != 64) return REHYAT_E_SHAPE;
+    if (!aligned(positions->data, positions->bits / 8)) return REHYAT_E_SHAPE;
+    if (positions->stride_b < 0 || positions->stride_n < 0) return REHYAT_E_SHAPE;
+    a.pos = positions->data;
+    a.pos_bits = positions->bits;
+    a.pos_b = positions->stride_b;
+    a.pos_n = positions->stride_n;
+    a.frame = a.cols = 1;
+  } else {
+    int64_t frame = 1;
+    if (axes > 1) {
+      if (positions->cols < 1 || (axes == 3 && positions->rows < 1)) return REHYAT_E_SHAPE;
+      frame = (int64_t)positions->cols * (axes == 3 ? positions->rows : 1);
+    }
+    a.frame = frame < N ? (uint32_t)frame : (uint32_t)N;   // a larger frame holds every token as well
+    a.cols = axes > 1 ? (uint32_t)positions->cols : 1;
+    a.start = (uint64_t)positions->start;
+  }
+  for (int i = 0; i < n_operands; ++i) {
+    const rehyat_rope_operand& o = operands[i];
+    if (!o.x || !o.out) return REHYAT_E_NULL;
+    if (o.heads < 1 || o.heads > 65535) return REHYAT_E_SHAPE;
+    if (!aligned(o.x, es) || !aligned(o.out, es)) return REHYAT_E_SHAPE;
+    const int64_t s[6] = {o.x_stride_b, o.x_stride_h, o.x_stride_n, o.out_stride_b, o.out_stride_h, o.out_stride_n};
+    for (int64_t v : s)
+      if (v < 0 || v >= ((int64_t)1 << 40)) return REHYAT_E_SHAPE;
+    if (!rows_apart(d, s[3], s[4], s[5], B, o.heads, N)) return REHYAT_E_SHAPE;
+    if (i == 1 && o.out == operands[0].out) return REHYAT_E_SHAPE;
+    a.op[i] = {o.x, o.out, s[0], s[1], s[2], s[3], s[4], s[5], o.heads};
+  }
+  a.turns = plan->turns;
+  a.rot = rot;
+  a.axes = axes;
+  a.sec1 = axes > 1 ? plan->section[0] : rot;
+  a.sec2 = axes > 2 ? plan->section[0] + plan->section[1] : rot;
+  a.scale = plan->scale;
+  a.sign = inverse ? -1.f : 1.f;
+  a.copies_from = rot / 2;
+  a.slots = rot / 2 + (d - rot);
+  a.N = N;
+  a.items = (uint32_t)B * N * a.slots;
+  a.group = 8;
+  a.groups0 = (a.op[0].heads + a.group - 1) / a.group;
+  const int groups = a.groups0 + (n_operands == 2 ? (a.op[1].heads + a.group - 1) / a.group : 0);
+  const dim3 grid((a.items + 255) / 256, groups);
+  hipStream_t st = (hipStream_t)stream;
+  switch (type) {
+    case REHYAT_BF16: launch<Bf16>(a, plan->layout, grid, st); break;
+    case REHYAT_FP16: launch<Fp16>(a, plan->layout, grid, st); break;
+    default: launch<Fp32>(a, plan->layout, grid, st);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return hip_fail(e, "rotary position kernel launch");
+  return REHYAT_OK;
+}
+
+}  // extern "C"

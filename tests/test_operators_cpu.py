@@ -1,0 +1,108 @@
+"""Refusals and host arithmetic of the operators around the attention, without a GPU: every rejected call returns before
+it touches the device (the pointers below are fake and never dereferenced)."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2601_04342_amd import binding
+
+A = 0x1000
+
+
+# ---- rotary positions ---------------------------------------------------------------------------------------------
+
+
+def rope_call(n_ops=1, B=2, N=8, type_=0, inverse=0, heads=3, x=A, out=2 * A, xs=None, os_=None, plan=None, pos=None,
+              second=None, **fields):
+    d = fields.get("d", 64)
+    p = binding.RopePlan(A, d, d, 0, 1, (ctypes.c_int32 * 3)(d // 2, 0, 0), 1.0)
+    if "d" in fields:
+        p.section[0] = fields.get("rot", d) // 2
+    for name, v in fields.items():
+        if name == "section":
+            p.section = (ctypes.c_int32 * 3)(*v)
+        else:
+            setattr(p, name, v)
+    ops = (binding.RopeOperand * 2)()
+    for i in range(2):
+        ops[i] = binding.RopeOperand(x, out + i * A, *(xs or (heads * N * d, N * d, d)), *(os_ or (heads * N * d, N * d, d)),
+                                     heads)
+    if second is not None:
+        for name, v in second.items():
+            setattr(ops[1], name, v)
+    return binding.library().rehyat_rope(ops, n_ops, ctypes.byref(p) if plan is None else plan,
+                                         ctypes.byref(binding.RopePositions() if pos is None else pos), B, N, type_,
+                                         inverse, None)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(n_ops=0), dict(n_ops=3), dict(B=0), dict(N=0), dict(type_=3), dict(type_=-1), dict(inverse=2),
+    dict(d=1, rot=2), dict(d=514), dict(rot=66), dict(rot=0), dict(rot=31), dict(layout=2), dict(axes=0), dict(axes=4),
+    dict(section=(31, 0, 0)), dict(axes=2, section=(32, 0, 0)), dict(axes=2, section=(33, -1, 0)), dict(scale=math.inf),
+    dict(scale=math.nan), dict(turns=A + 4), dict(x=A + 1), dict(out=A + 1), dict(type_=2, x=A + 2), dict(heads=0),
+    dict(heads=65536), dict(xs=(-1, 512, 64)), dict(xs=(1536, 512, 1 << 40)), dict(os_=(1536, 512, 32)),
+    dict(os_=(1536, 0, 64)), dict(os_=(0, 512, 64)), dict(os_=(1500, 512, 64)), dict(B=1 << 16, N=1 << 15),
+    dict(B=1 << 15, N=1 << 10), dict(n_ops=2, second=dict(out=2 * A)), dict(n_ops=2, second=dict(heads=0)),
+])
+def test_rope_rejects(bad):
+    assert rope_call(**bad) == binding.E_SHAPE
+
+
+def test_rope_rejects_null_and_bad_positions():
+    lib = binding.library()
+    assert rope_call(turns=None) == binding.E_NULL
+    assert rope_call(x=None) == binding.E_NULL
+    assert rope_call(n_ops=2, second=dict(out=None)) == binding.E_NULL
+    assert lib.rehyat_rope(None, 1, None, None, 1, 1, 0, 0, None) == binding.E_NULL
+    P = binding.RopePositions
+    three = dict(axes=3, section=(12, 10, 10))
+    for pos in (P(rows=3), P(cols=4), P(rows=-1, cols=4)):
+        assert rope_call(pos=pos, **three) == binding.E_SHAPE
+    assert rope_call(pos=P(cols=0), axes=2, section=(16, 16, 0)) == binding.E_SHAPE
+    for pos in (P(data=A, bits=16), P(data=A + 4, bits=64), P(data=A + 2, bits=32), P(data=A, bits=32, stride_b=-1),
+                P(data=A, bits=32, stride_n=-1)):
+        assert rope_call(pos=pos) == binding.E_SHAPE
+
+
+def test_turns_are_the_frequencies_modulo_a_turn():
+    lib = binding.library()
+
+    def turns(*radians):
+        f = (ctypes.c_double * len(radians))(*radians)
+        t = (ctypes.c_uint64 * len(radians))()
+        return lib.rehyat_rope_turns(f, len(radians), t), list(t)
+
+    rc, t = turns(0.0, 1.0, -1.0, math.pi, 2 * math.pi, 100.0, 1e-12)
+    assert rc == binding.OK
+    # an x87 quotient is off by at most half of 2^-63 of itself; math.pi as a double is 1.2e-16 off pi
+    one = 2**64 / (2 * math.pi)
+    assert t[0] == 0 and abs(t[1] - one) <= 2**64 * 2.0**-53 and t[1] + t[2] in (2**64 - 1, 2**64, 2**64 + 1)
+    assert abs(t[3] - 2**63) <= 2**64 * 2.0**-53 and min(t[4], 2**64 - t[4]) <= 2**64 * 2.0**-52
+    assert abs(t[5] - (100 / (2 * math.pi) % 1) * 2**64) <= 2**64 * 2.0**-47 and abs(t[6] - 1e-12 * one) <= 1
+    assert turns(math.nan)[0] == binding.E_SHAPE and turns(1.0, math.inf)[0] == binding.E_SHAPE
+    assert lib.rehyat_rope_turns(None, 1, (ctypes.c_uint64 * 1)()) == binding.E_NULL
+    assert lib.rehyat_rope_turns((ctypes.c_double * 1)(), 0, (ctypes.c_uint64 * 1)()) == binding.E_SHAPE
+
+
+@pytest.mark.parametrize("bad", [
+    dict(rot=3), dict(rot=0), dict(rot=130), dict(layout="other"), dict(sections=(32, 31)), dict(sections=(64, 0)),
+    dict(sections=(16, 16, 16, 16)), dict(scaling=dict(kind="no", factor=2.0)), dict(scaling=dict(kind="linear", factor=0.0)),
+    dict(scaling=dict(kind="parts", factor=2.0, original=100, low=2, high=2)), dict(freqs=[1.0]),
+    dict(freqs=[1.0] * 64, scaling=dict(kind="linear", factor=2.0)),
+])
+def test_rope_plan_rejects(bad):
+    with pytest.raises(ValueError):
+        binding.Rope(128, device="cpu", **bad)
+
+
+def test_video_plan_splits_the_pairs():
+    for d, want in ((128, (22, 21, 21)), (64, (12, 10, 10)), (6, (1, 1, 1))):
+        assert binding.Rope.video(d, device="cpu").sections == want
+
+
+def test_rope_binding_rejects_host_tensors_and_missing_grids():
+    plan = binding.Rope(64, device="cpu")
+    with pytest.raises(TypeError):
+        binding.rope(torch.zeros(1, 2, 8, 64, dtype=torch.bfloat16), None, plan)
