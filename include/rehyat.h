@@ -392,6 +392,31 @@ int rehyat_rope(const rehyat_rope_operand *operands, int n_operands,
                 int inverse, void *stream);
 
 /*
+ * The loss of the attention distillation (Eq. 19) and its gradient, in one pass:
+ *     E = scale * sum_i w_i |y_hat_i - y_i| ,  G = scale * w_i * sign(y_hat_i - y_i)
+ *   y_hat   [B, H, N, d] bf16 DEVICE, the student's output (rehyat_forward)
+ *   y       same shape, of `type`: the teacher's
+ *   weight  [B, N] fp32 DEVICE, nullable (1): a factor for each token.  Where it
+ *           is 0, G is 0 and the elements do not count, whatever they hold (the
+ *           padding of a batch).
+ *   scale   1 / (number of elements that count) gives the mean of Eq. 19
+ *   grad    same shape, bf16, overwritten: grad_out of rehyat_phi_backward.  NaN
+ *           where y_hat or y is.
+ *   loss    one fp32, DEVICE, overwritten
+ * |y_hat - y| is formed in fp32 and summed in fp64 in a fixed order.
+ * y_hat, y and grad 16-byte aligned, weight and loss 4-byte; grad overlaps no input.
+ * workspace: DEVICE, 256-byte aligned, rehyat_distill_loss_workspace_bytes(...)
+ * bytes; nothing in it is assumed or survives.
+ * Supported: B * H <= 65535, N * d < 2^31.
+ * Errors: REHYAT_E_NULL, REHYAT_E_SHAPE, REHYAT_E_WORKSPACE.
+ */
+size_t rehyat_distill_loss_workspace_bytes(int B, int H, int N, int d);
+int rehyat_distill_loss(const void *y_hat, const void *y, int type,
+                        const float *weight, float scale, void *grad,
+                        float *loss, int B, int H, int N, int d,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Running state of the chunk-wise RNN (Eq. 14-15, 17-18) after absorbing
  * tokens [0, upto) of every head, as the state kernels compute it:
  *   S_out [B, H, dprime, d] fp32,  z_out [B, H, dprime] fp32  (DEVICE)

@@ -24,6 +24,7 @@ EXPORTS = ("rehyat_chunk_plan", "rehyat_workspace_bytes", "rehyat_set_workspace"
            "rehyat_step", "rehyat_state", "rehyat_shutdown",
            "rehyat_phi_backward", "rehyat_phi_backward_workspace_bytes",
            "rehyat_rope", "rehyat_rope_turns",
+           "rehyat_distill_loss", "rehyat_distill_loss_workspace_bytes",
            "rehyat_status_string", "rehyat_version", "rehyat_last_hip_error",
            "rehyat_attn_kernel_name",
            "rehyat_profile_enable", "rehyat_profile_read", "rehyat_debug_set_xcd_mask")
@@ -131,6 +132,11 @@ def _load():
     lib.rehyat_rope.restype = ci
     lib.rehyat_rope.argtypes = [ctypes.POINTER(RopeOperand), ci, ctypes.POINTER(RopePlan),
                                 ctypes.POINTER(RopePositions), ci, ci, ci, ci, vp]
+    lib.rehyat_distill_loss_workspace_bytes.restype = ctypes.c_size_t
+    lib.rehyat_distill_loss_workspace_bytes.argtypes = [ci, ci, ci, ci]
+    lib.rehyat_distill_loss.restype = ci
+    lib.rehyat_distill_loss.argtypes = [vp, vp, ci, vp, ctypes.c_float, vp, vp, ci, ci, ci, ci, vp,
+                                        ctypes.c_size_t, vp]
     lib.rehyat_shutdown.restype = ci
     lib.rehyat_shutdown.argtypes = []
     lib.rehyat_status_string.restype = ctypes.c_char_p
@@ -597,3 +603,52 @@ def rope(q, k, plan, grid=None, start=0, positions=None, inverse=False, out=None
     if rc != OK:
         raise RehyatError(rc, "rehyat_rope")
     return q_out if k is None else (q_out, k_out)
+
+
+def distill_loss_workspace_bytes(B, H, N, d):
+    return _load().rehyat_distill_loss_workspace_bytes(B, H, N, d)
+
+
+def distill_loss(y_hat, y, scale=None, weight=None, grad=None, loss=None, workspace=None, stream=None):
+    """The loss of Eq. 19, scale * sum weight |y_hat - y|, and its gradient with respect to y_hat (bf16, what
+    ``phi_backward`` takes as ``grad_out``).  y_hat: CUDA bf16 [B, H, N, d]; y: the same shape in bf16, fp16 or fp32;
+    ``weight``: fp32 [B, N], 0 for tokens that do not count, whatever they hold.  ``scale`` is 1 / (number of elements)
+    by default.  ``workspace``: a CUDA byte tensor of ``distill_loss_workspace_bytes`` (allocated here if None).
+    Returns ``(loss, grad)``: one fp32 on the device, and a bf16 tensor like y_hat."""
+    ctx = _elsewhere(y_hat, stream) if y_hat.is_cuda else None
+    if ctx is not None:
+        with ctx:
+            return distill_loss(y_hat, y, scale, weight, grad, loss, workspace)
+    lib = _load()
+    if y_hat.dtype != torch.bfloat16 or not y_hat.is_cuda or not y_hat.is_contiguous() or y_hat.dim() != 4:
+        raise TypeError("y_hat must be a contiguous CUDA bf16 tensor [B, H, N, d]")
+    dev = y_hat.device
+    if y.dtype not in _TYPES or y.device != dev or not y.is_contiguous():
+        raise TypeError("y must be a contiguous CUDA tensor in bf16, fp16 or fp32 on y_hat's device")
+    if y.shape != y_hat.shape:
+        raise ValueError("y_hat and y shapes differ")
+    B, H, N, d = y_hat.shape
+    if weight is not None and (weight.dtype != torch.float32 or weight.device != dev or not weight.is_contiguous()
+                               or weight.shape != (B, N)):
+        raise TypeError("weight must be a contiguous CUDA fp32 tensor [B, N]")
+    if grad is None:
+        grad = torch.empty_like(y_hat)
+    elif grad.shape != y_hat.shape or grad.dtype != torch.bfloat16 or grad.device != dev or not grad.is_contiguous():
+        raise TypeError("grad must be a contiguous CUDA bf16 tensor like y_hat")
+    if loss is None:
+        loss = torch.empty((), device=dev, dtype=torch.float32)
+    elif loss.numel() != 1 or loss.dtype != torch.float32 or loss.device != dev:
+        raise TypeError("loss must be one CUDA fp32")
+    if workspace is None:
+        workspace = torch.empty(lib.rehyat_distill_loss_workspace_bytes(B, H, N, d), device=dev, dtype=torch.uint8)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise TypeError("workspace must be a contiguous tensor on y_hat's device")
+    if scale is None:
+        scale = 1.0 / max(1, y_hat.numel())
+    rc = lib.rehyat_distill_loss(y_hat.data_ptr(), y.data_ptr(), _TYPES[y.dtype],
+                                 None if weight is None else weight.data_ptr(), scale, grad.data_ptr(), loss.data_ptr(),
+                                 B, H, N, d, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                 _stream_handle(None))
+    if rc != OK:
+        raise RehyatError(rc, "rehyat_distill_loss")
+    return loss, grad

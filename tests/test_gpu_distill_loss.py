@@ -1,0 +1,192 @@
+"""The distillation loss (rehyat_distill_loss) against its formula in 64 bits: types, ragged sizes, weights that leave
+tokens or everything out, what is not a number, streams and graphs."""
+import pytest
+import torch
+
+from paper_2601_04342_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+BF16 = torch.bfloat16
+
+
+def inputs(B, H, N, d, teacher, seed, spread=0.1):
+    g = torch.Generator().manual_seed(seed)
+    y = torch.randn(B, H, N, d, generator=g).to(teacher)
+    y_hat = (y.float() + spread * torch.randn(B, H, N, d, generator=g)).to(BF16)
+    return y_hat, y
+
+
+def reference(y_hat, y, scale, weight=None):
+    diff = y_hat.double() - y.double()
+    w = torch.ones(diff.shape[0], 1, diff.shape[2], 1, dtype=torch.float64) if weight is None else \
+        weight.double()[:, None, :, None]
+    diff = torch.where(w == 0, 0.0, diff)
+    return (w * diff.abs()).sum() * scale, scale * w * diff.sign()
+
+
+def check(loss, grad, y_hat, y, scale, weight=None):
+    want, g = reference(y_hat, y, scale, weight)
+    # differences and their products with a weight are rounded to 24 bits, up to 8 of them are added in 32 bits (7
+    # roundings of partial sums), sums of those and the total in 53; the loss is rounded once, the scale to 24 bits
+    assert abs(loss.item() - want.item()) <= (2 + 7 + 2) * 2.0**-24 * abs(want.item()), (loss.item(), want.item())
+    # the gradient is exact but for the rounding of scale and product to 24 bits and one rounding to bf16
+    err = (grad.cpu().double() - g).abs()
+    assert (err <= (2.0**-8 + 2 * 2.0**-24) * (1 + 2.0**-8) * g.abs()).all()
+    assert torch.equal(grad.cpu() == 0, g == 0)
+
+
+def run(B, H, N, d, teacher=BF16, weight=None, scale=None, seed=0):
+    y_hat, y = inputs(B, H, N, d, teacher, seed)
+    dw = None if weight is None else weight.cuda()
+    grad = torch.full((B, H, N, d), float("nan"), device="cuda", dtype=BF16)
+    loss, out = binding.distill_loss(y_hat.cuda(), y.cuda(), scale=scale, weight=dw, grad=grad)
+    assert out is grad and loss.shape == ()
+    check(loss, grad, y_hat, y, 1.0 / y.numel() if scale is None else scale, weight)
+
+
+SHAPES = [(1, 1, 1, 1), (1, 1, 1, 7), (1, 2, 256, 64), (1, 12, 100, 128), (3, 2, 77, 128), (2, 3, 1, 64), (1, 1, 5, 3),
+          (2, 5, 333, 10), (1, 1, 4097, 64), (1, 3, 2731, 33), (300, 7, 2, 8), (1, 1, 70001, 17), (40, 100, 1, 4)]
+
+
+@pytest.mark.parametrize("weighted", [False, True])
+@pytest.mark.parametrize("teacher", [BF16, torch.float16, torch.float32])
+@pytest.mark.parametrize("B,H,N,d", SHAPES)
+def test_shapes_and_types(B, H, N, d, teacher, weighted):
+    weight = None
+    if weighted:
+        g = torch.Generator().manual_seed(N)
+        weight = torch.rand(B, N, generator=g) * (torch.rand(B, N, generator=g) < 0.7)
+    run(B, H, N, d, teacher, weight, seed=B + N)
+
+
+def test_full_size():
+    """One layer at 480x832, 21 latent frames."""
+    run(1, 12, 32760, 128, seed=1)
+
+
+@pytest.mark.parametrize("scale", [1.0, -2.5, 0.0, 1e-9, 3e38])
+def test_scales(scale):
+    y_hat, y = inputs(1, 2, 50, 64, BF16, 2)
+    loss, grad = binding.distill_loss(y_hat.cuda(), y.cuda(), scale=scale)
+    if scale < 1e38:
+        check(loss, grad, y_hat, y, scale)
+    else:
+        assert torch.isinf(loss) and torch.isfinite(grad.float()).all()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("side", ["y_hat", "y"])
+def test_tokens_of_weight_zero_do_not_count_whatever_they_hold(side, bad):
+    B, H, N, d = 2, 3, 40, 64
+    y_hat, y = inputs(B, H, N, d, torch.float32, 3)
+    weight = torch.ones(B, N)
+    weight[0, 30:] = 0
+    weight[1, :7] = 0
+    weight[1, 20] = 0
+    want, g = reference(y_hat, y, 0.5, weight)
+    t = {"y_hat": y_hat, "y": y}[side]
+    t.masked_fill_((weight == 0)[:, None, :, None], bad)
+    loss, grad = binding.distill_loss(y_hat.cuda(), y.cuda(), scale=0.5, weight=weight.cuda())
+    assert abs(loss.item() - want.item()) <= 11 * 2.0**-24 * want.item()
+    assert torch.equal(grad.cpu().double(), g)   # 0.5 and 1 are exact
+
+
+def test_nothing_counts():
+    y_hat, y = inputs(2, 2, 9, 64, BF16, 4)
+    loss, grad = binding.distill_loss(y_hat.cuda(), y.cuda(), weight=torch.zeros(2, 9, device="cuda"))
+    assert loss.item() == 0 and (grad == 0).all()
+
+
+def test_what_is_not_a_number_shows():
+    y_hat, y = inputs(1, 2, 30, 64, BF16, 5)
+    y_hat[0, 1, 3, 5] = float("nan")
+    y[0, 0, 2, 63] = float("inf")
+    y_hat[0, 0, 9, 1] = float("inf")
+    y[0, 0, 9, 1] = float("inf")        # inf - inf
+    loss, grad = binding.distill_loss(y_hat.cuda(), y.cuda(), scale=1.0)
+    assert torch.isnan(loss)
+    nan = torch.zeros_like(y_hat, dtype=torch.bool)
+    nan[0, 1, 3, 5] = nan[0, 0, 9, 1] = True
+    assert torch.equal(torch.isnan(grad.cpu()), nan) and grad[0, 0, 2, 63] == -1
+    keep = ~nan
+    assert torch.equal(grad.cpu().double()[keep], (y_hat.double() - y.double()).sign()[keep])
+
+
+def test_equal_values_have_no_gradient():
+    y_hat, _ = inputs(1, 1, 30, 64, BF16, 6)
+    loss, grad = binding.distill_loss(y_hat.cuda(), y_hat.float().cuda())
+    assert loss.item() == 0 and (grad == 0).all()
+
+
+def test_gradient_against_differences():
+    y_hat, y = inputs(1, 2, 8, 16, torch.float32, 7, spread=1.0)
+    w = torch.rand(1, 8, generator=torch.Generator().manual_seed(8))
+    _, grad = binding.distill_loss(y_hat.cuda(), y.cuda(), scale=1.0, weight=w.cuda())
+    for h, n, c in ((0, 0, 0), (1, 7, 15), (0, 3, 8), (1, 4, 2)):
+        at = []
+        for step in (-2.0**-6, 2.0**-6):
+            e = y_hat.double()
+            e[0, h, n, c] += step
+            at.append(reference(e, y, 1.0, w)[0])
+        if (y_hat[0, h, n, c] - y[0, h, n, c]).abs() > 2.0**-6:
+            slope = (at[1] - at[0]).item() / 2.0**-5
+            assert abs(slope - grad[0, h, n, c].item()) <= 2.0**-8 * 1.01 * abs(slope) + 1e-9
+
+
+def test_repeatable_and_only_outputs_are_written():
+    B, H, N, d = 1, 3, 1111, 64
+    y_hat, y = (t.cuda() for t in inputs(B, H, N, d, torch.float32, 9))
+    w = torch.rand(B, N, device="cuda")
+    keep = [t.clone() for t in (y_hat, y, w)]
+    need = binding.distill_loss_workspace_bytes(B, H, N, d)
+    store = torch.full((need + 512,), 0xAB, device="cuda", dtype=torch.uint8)
+    ws = store[256:256 + need]
+    losses, grads = zip(*(binding.distill_loss(y_hat, y, weight=w, workspace=ws) for _ in range(5)))
+    assert all(torch.equal(x, losses[0]) for x in losses) and all(torch.equal(x, grads[0]) for x in grads)
+    assert all(torch.equal(a, b) for a, b in zip(keep, (y_hat, y, w)))
+    assert (store[:256] == 0xAB).all() and (store[256 + need:] == 0xAB).all()
+
+
+def test_streams_and_graph():
+    y_hat, y = (t.cuda() for t in inputs(2, 3, 700, 128, BF16, 10))
+    want, g = binding.distill_loss(y_hat, y)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other, go = binding.distill_loss(y_hat, y, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(other, want) and torch.equal(go, g)
+    loss, grad = torch.zeros((), device="cuda"), torch.zeros_like(y_hat)
+    ws = torch.empty(binding.distill_loss_workspace_bytes(2, 3, 700, 128), device="cuda", dtype=torch.uint8)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.distill_loss(y_hat, y, loss=loss, grad=grad, workspace=ws)
+    for i in range(3):
+        loss.fill_(float("nan"))
+        grad.fill_(float("nan"))
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(loss, want) and torch.equal(grad, g), i
+        binding.distill_loss(y, y_hat)
+
+
+def test_refusals():
+    y_hat, y = (t.cuda() for t in inputs(1, 2, 8, 64, BF16, 11))
+    for bad in (dict(weight=torch.ones(1, 7, device="cuda")), dict(weight=torch.ones(1, 8, device="cuda").half()),
+                dict(weight=torch.ones(1, 8)), dict(grad=torch.empty_like(y_hat, dtype=torch.float32)),
+                dict(grad=torch.empty_like(y_hat[:, :1])), dict(loss=torch.zeros(2, device="cuda"))):
+        with pytest.raises(TypeError):
+            binding.distill_loss(y_hat, y, **bad)
+    with pytest.raises(ValueError):
+        binding.distill_loss(y_hat, y[:, :1].contiguous())
+    with pytest.raises(TypeError):
+        binding.distill_loss(y_hat, y.double())
+    with pytest.raises(TypeError):
+        binding.distill_loss(y_hat.float(), y)
+    with pytest.raises(binding.RehyatError) as e:
+        binding.distill_loss(y_hat, y, workspace=torch.empty(8, device="cuda", dtype=torch.uint8))
+    assert e.value.code == binding.E_WORKSPACE
+    torch.cuda.synchronize()

@@ -106,3 +106,37 @@ def test_rope_binding_rejects_host_tensors_and_missing_grids():
     plan = binding.Rope(64, device="cpu")
     with pytest.raises(TypeError):
         binding.rope(torch.zeros(1, 2, 8, 64, dtype=torch.bfloat16), None, plan)
+
+
+# ---- distillation loss --------------------------------------------------------------------------------------------
+
+
+def loss_call(y_hat=A, y=2 * A, type_=0, weight=None, scale=1.0, grad=3 * A, loss=A, B=1, H=2, N=8, d=64, ws=A, bytes_=1 << 20):
+    return binding.library().rehyat_distill_loss(y_hat, y, type_, weight, scale, grad, loss, B, H, N, d, ws, bytes_, None)
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(y_hat=None), "NULL"), (dict(y=None), "NULL"), (dict(grad=None), "NULL"), (dict(loss=None), "NULL"),
+    (dict(ws=None), "NULL"), (dict(type_=3), "SHAPE"), (dict(scale=math.nan), "SHAPE"), (dict(scale=math.inf), "SHAPE"),
+    (dict(y_hat=A + 8), "SHAPE"), (dict(y=A + 2), "SHAPE"), (dict(grad=A + 4), "SHAPE"), (dict(loss=A + 2), "SHAPE"),
+    (dict(weight=A + 1), "SHAPE"), (dict(B=0), "SHAPE"), (dict(H=0), "SHAPE"), (dict(N=0), "SHAPE"), (dict(d=0), "SHAPE"),
+    (dict(B=256, H=256), "SHAPE"), (dict(N=1 << 24, d=128), "SHAPE"), (dict(ws=A + 16), "WORKSPACE"),
+    (dict(bytes_=0), "WORKSPACE"),
+])
+def test_distill_loss_rejects(bad, code):
+    assert loss_call(**bad) == getattr(binding, "E_" + code)
+
+
+def test_distill_loss_workspace():
+    size = binding.distill_loss_workspace_bytes
+    for shape in ((1, 1, 1, 1), (1, 12, 32760, 128), (65535, 1, 1, 1), (2, 12, 75600, 128), (255, 257, 3000, 64)):
+        need = size(*shape)
+        assert need % 256 == 0 and 0 < need <= 1 << 20
+        assert loss_call(B=shape[0], H=shape[1], N=shape[2], d=shape[3], bytes_=need - 1) == binding.E_WORKSPACE
+    assert size(0, 1, 1, 1) == size(1, 1, 1 << 24, 128) == size(256, 256, 1, 1) == 0
+
+
+def test_distill_loss_binding_rejects_host_tensors():
+    y = torch.zeros(1, 2, 8, 64, dtype=torch.bfloat16)
+    with pytest.raises(TypeError):
+        binding.distill_loss(y, y)
