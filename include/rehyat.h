@@ -417,6 +417,83 @@ int rehyat_distill_loss(const void *y_hat, const void *y, int type,
                         void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * AdamW over many tensors in one launch: the update behind rehyat_phi_backward,
+ * for the feature maps of one block or of all of them.  With t the number of this
+ * update and g the gradient
+ *     m = beta1 m + (1 - beta1) g ,  v = beta2 v + (1 - beta2) g^2
+ *     p = p (1 - lr weight_decay)
+ *         - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32.
+ *
+ * rehyat_adamw_tensor (HOST struct of DEVICE pointers)
+ *   param, param_type   n elements, REHYAT_BF16 / FP16 / FP32, read (where there is
+ *                       no master) and written
+ *   master              n fp32, nullable: p itself, of which param is then the
+ *                       rounded copy.  Without it p is rounded to param_type at
+ *                       every step, and a change of less than half a rounding
+ *                       step of p is lost.
+ *   grad, grad_type     n elements, read
+ *   m, v                state_bits 32: n fp32 each.
+ *                       state_bits 8: one byte an element, n rounded up to a
+ *                       multiple of 32 of them, with one byte of exponent for
+ *                       each group of 32 elements in m_exp, v_exp (ceil(n / 32)
+ *                       bytes); all zero to begin with.  Bytes of m are e4m3
+ *                       numbers, to be multiplied by 2^(m_exp - 134).  A byte c > 0
+ *                       of v is an fp32 number without sign whose leading 11 bits
+ *                       are c + 8 (v_exp - 30); 0 is 0.  Exponent 255: no element
+ *                       of the group is a number any more (a gradient was not
+ *                       finite, or a moment passed 2^127).
+ *                       The new moments are rounded once to fp32 (so from 1 - beta1
+ *                       and 1 - beta2 in fp32), enter the update, and are rounded
+ *                       from there to 8 bits, to nearest; a v that is not 0 never
+ *                       becomes 0.
+ * Pointers are aligned to their elements, m and v to 16 bytes.  Ranges that are
+ * written overlap no other range of any tensor.
+ *
+ * rehyat_adamw_prepare writes what a step needs to know of the tensors into `table`
+ * (DEVICE, 256-byte aligned, rehyat_adamw_table_bytes() bytes), enqueued on `stream`, and
+ * fills *plan (HOST).  The table holds the pointers: prepare again when a tensor
+ * has moved.  Its first 8 bytes are the number of updates made so far (int64,
+ * `step` to begin with; the caller may read or set it, ordered on the stream), which every
+ * step increments on the device, so a step that is captured in a graph counts on
+ * with every replay.
+ * rehyat_adamw_step: one update of all tensors.  lr_device (DEVICE fp32, nullable)
+ * replaces lr, for schedules under replay.  Steps of one table must be ordered.
+ * rehyat_adamw_moments: the values of 8-bit moments of n elements (DEVICE fp32 out,
+ * 16-byte aligned).
+ * Errors: REHYAT_E_NULL, REHYAT_E_SHAPE (also: overlapping ranges; lr, eps or
+ * weight_decay negative or not finite, eps 0, a beta outside [0, 1)), REHYAT_E_WORKSPACE.
+ */
+typedef struct {
+  void *param;
+  float *master;
+  const void *grad;
+  void *m, *v;
+  void *m_exp, *v_exp;
+  int64_t n;
+  int32_t param_type, grad_type;
+} rehyat_adamw_tensor;
+typedef struct {
+  void *table;
+  int64_t items; /* pieces of work */
+  int32_t n_tensors, state_bits;
+} rehyat_adamw_plan;
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;
+  const float *lr_device;
+} rehyat_adamw_hyper;
+size_t rehyat_adamw_table_bytes(const int64_t *sizes, int n_tensors);
+int rehyat_adamw_prepare(const rehyat_adamw_tensor *tensors, int n_tensors,
+                         int state_bits, int64_t step, void *table,
+                         size_t table_bytes, rehyat_adamw_plan *plan,
+                         void *stream);
+int rehyat_adamw_step(const rehyat_adamw_plan *plan,
+                      const rehyat_adamw_hyper *hyper, void *stream);
+int rehyat_adamw_moments(const void *m, const void *m_exp, const void *v,
+                         const void *v_exp, float *m_out, float *v_out,
+                         int64_t n, void *stream);
+
+/*
  * Running state of the chunk-wise RNN (Eq. 14-15, 17-18) after absorbing
  * tokens [0, upto) of every head, as the state kernels compute it:
  *   S_out [B, H, dprime, d] fp32,  z_out [B, H, dprime] fp32  (DEVICE)

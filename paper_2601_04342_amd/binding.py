@@ -25,6 +25,7 @@ EXPORTS = ("rehyat_chunk_plan", "rehyat_workspace_bytes", "rehyat_set_workspace"
            "rehyat_phi_backward", "rehyat_phi_backward_workspace_bytes",
            "rehyat_rope", "rehyat_rope_turns",
            "rehyat_distill_loss", "rehyat_distill_loss_workspace_bytes",
+           "rehyat_adamw_table_bytes", "rehyat_adamw_prepare", "rehyat_adamw_step", "rehyat_adamw_moments",
            "rehyat_status_string", "rehyat_version", "rehyat_last_hip_error",
            "rehyat_attn_kernel_name",
            "rehyat_profile_enable", "rehyat_profile_read", "rehyat_debug_set_xcd_mask")
@@ -70,6 +71,21 @@ class RopePositions(ctypes.Structure):
 class RopeOperand(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p)] + [
         (f"{t}_stride_{n}", ctypes.c_int64) for t in ("x", "out") for n in "bhn"] + [("heads", ctypes.c_int32)]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "master", "grad", "m", "v", "m_exp", "v_exp")] + [
+        ("n", ctypes.c_int64), ("param_type", ctypes.c_int32), ("grad_type", ctypes.c_int32)]
+
+
+class AdamWPlan(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("items", ctypes.c_int64), ("n_tensors", ctypes.c_int32),
+                ("state_bits", ctypes.c_int32)]
+
+
+class AdamWHyper(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [
+        ("lr_device", ctypes.c_void_p)]
 
 
 class RehyatError(RuntimeError):
@@ -137,6 +153,15 @@ def _load():
     lib.rehyat_distill_loss.restype = ci
     lib.rehyat_distill_loss.argtypes = [vp, vp, ci, vp, ctypes.c_float, vp, vp, ci, ci, ci, ci, vp,
                                         ctypes.c_size_t, vp]
+    lib.rehyat_adamw_table_bytes.restype = ctypes.c_size_t
+    lib.rehyat_adamw_table_bytes.argtypes = [ctypes.POINTER(ctypes.c_int64), ci]
+    lib.rehyat_adamw_prepare.restype = ci
+    lib.rehyat_adamw_prepare.argtypes = [ctypes.POINTER(AdamWTensor), ci, ci, ctypes.c_int64, vp, ctypes.c_size_t,
+                                         ctypes.POINTER(AdamWPlan), vp]
+    lib.rehyat_adamw_step.restype = ci
+    lib.rehyat_adamw_step.argtypes = [ctypes.POINTER(AdamWPlan), ctypes.POINTER(AdamWHyper), vp]
+    lib.rehyat_adamw_moments.restype = ci
+    lib.rehyat_adamw_moments.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.c_int64, vp]
     lib.rehyat_shutdown.restype = ci
     lib.rehyat_shutdown.argtypes = []
     lib.rehyat_status_string.restype = ctypes.c_char_p
@@ -652,3 +677,169 @@ def distill_loss(y_hat, y, scale=None, weight=None, grad=None, loss=None, worksp
     if rc != OK:
         raise RehyatError(rc, "rehyat_distill_loss")
     return loss, grad
+
+
+def _leaves(x):
+    """The tensors of nested dicts, lists and tuples, in order."""
+    if isinstance(x, torch.Tensor):
+        return [x]
+    return [t for v in (x.values() if isinstance(x, dict) else x) for t in _leaves(v)]
+
+
+def _like(x, tensors):
+    """The structure of ``x`` with the tensors of an iterator in it."""
+    if isinstance(x, torch.Tensor):
+        return next(tensors)
+    return {n: _like(v, tensors) for n, v in x.items()} if isinstance(x, dict) else [_like(v, tensors) for v in x]
+
+
+def _offsets(sizes, step=256):
+    """Where each of these many elements begins in one buffer, at multiples of ``step``; and the buffer's size."""
+    out, at = [], 0
+    for n in sizes:
+        out.append(at)
+        at += -(-n // step) * step
+    return out, at
+
+
+class AdamW:
+    """AdamW over all of ``params`` (tensors in nested dicts and lists: the phi of one block, or a list of the phi of
+    all; CUDA, contiguous, bf16 / fp16 / fp32), one launch a step.
+
+    ``grads``, of the same structure and shapes, in bf16, fp16 or fp32, are what a step reads; without them fp32 ones
+    are made, to be written by ``phi_backward(grads=opt.grads)``.  ``master=True`` keeps an fp32 copy of parameters that
+    are not fp32, which is what is updated (``reset_master`` after a change of the parameters from elsewhere).
+    ``state_bits``: 32, or 8 for moments in 8 bits under an exponent for each 32 elements.
+
+    ``lr``, ``betas``, ``eps`` and ``weight_decay`` may be set between steps.  State: ``m``, ``v`` (fp32, or e4m3 and
+    uint8 with ``m_exp``, ``v_exp``), each one buffer in which tensor i begins at ``offsets[i]``; ``master``, likewise at
+    ``master_offsets[i]`` (None: no copy); ``step_count``, on the device."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, master=True,
+                 grads=None):
+        self.params = _leaves(params)
+        self.lr, self.betas, self.eps, self.weight_decay, self.state_bits = lr, betas, eps, weight_decay, state_bits
+        if not self.params:
+            raise ValueError("no parameters")
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        dev = self.params[0].device
+        for p in self.params:
+            if p.dtype not in _TYPES or not p.is_cuda or p.device != dev or not p.is_contiguous():
+                raise TypeError("parameters must be contiguous CUDA tensors in bf16, fp16 or fp32 on one device")
+        with torch.cuda.device(dev):
+            self._allocate(params, grads, bool(master), dev)
+            self._prepare(0)
+
+    def _allocate(self, params, grads, master, dev):
+        sizes = [p.numel() for p in self.params]
+        self.offsets, total = _offsets(sizes)
+        zeros = lambda n, dtype: torch.zeros(n, device=dev, dtype=dtype)
+        if grads is None:
+            flat = zeros(total, torch.float32)
+            self._grads = [flat[o:o + n].view(p.shape) for o, n, p in zip(self.offsets, sizes, self.params)]
+            self.grads = _like(params, iter(self._grads))
+        else:
+            self._grads, self.grads = _leaves(grads), grads
+            if len(self._grads) != len(self.params):
+                raise ValueError("grads must have a tensor for each parameter")
+            for p, g in zip(self.params, self._grads):
+                if g.dtype not in _TYPES or g.device != dev or not g.is_contiguous() or g.shape != p.shape:
+                    raise TypeError("grads must be contiguous CUDA tensors shaped like the parameters")
+        if self.state_bits == 32:
+            self.m, self.v = zeros(total, torch.float32), zeros(total, torch.float32)
+            self.m_exp = self.v_exp = None
+        else:
+            self.m, self.v = zeros(total, torch.float8_e4m3fn), zeros(total, torch.uint8)
+            self.m_exp, self.v_exp = zeros(total // 32, torch.uint8), zeros(total // 32, torch.uint8)
+        held = [n if master and p.dtype != torch.float32 else None for p, n in zip(self.params, sizes)]
+        at, total = _offsets([n or 0 for n in held])
+        self.master_offsets = [o if n is not None else None for o, n in zip(at, held)]
+        self.master = zeros(total, torch.float32) if total else None
+        self.reset_master()
+
+    def reset_master(self):
+        """The fp32 copies <- the parameters as they are now."""
+        for p, o in zip(self.params, self.master_offsets):
+            if o is not None:
+                self.master[o:o + p.numel()].copy_(p.view(-1))
+
+    def _prepare(self, step):
+        n = len(self.params)
+        tensors, sizes = (AdamWTensor * n)(), (ctypes.c_int64 * n)()
+        at = lambda buffer, element: None if buffer is None else buffer.data_ptr() + element * buffer.element_size()
+        for i, (p, g, o, mo) in enumerate(zip(self.params, self._grads, self.offsets, self.master_offsets)):
+            sizes[i] = p.numel()
+            tensors[i] = AdamWTensor(p.data_ptr(), None if mo is None else at(self.master, mo), g.data_ptr(),
+                                     at(self.m, o), at(self.v, o), at(self.m_exp, o // 32), at(self.v_exp, o // 32),
+                                     p.numel(), _TYPES[p.dtype], _TYPES[g.dtype])
+        lib = _load()
+        need = lib.rehyat_adamw_table_bytes(sizes, n)
+        if need == 0:
+            raise RehyatError(E_SHAPE, "rehyat_adamw_table_bytes")
+        self._table = torch.empty(need, device=self.m.device, dtype=torch.uint8)
+        self.step_count = self._table[:8].view(torch.int64).view(())
+        self._plan, self._hyper = AdamWPlan(), AdamWHyper()
+        rc = lib.rehyat_adamw_prepare(tensors, n, self.state_bits, step, self._table.data_ptr(), need,
+                                      ctypes.byref(self._plan), _stream_handle(None))
+        if rc != OK:
+            raise RehyatError(rc, "rehyat_adamw_prepare")
+
+    def step(self, lr=None, stream=None):
+        """One update of every parameter from ``grads``.  ``lr``: a number for this step, or one fp32 on the device,
+        which a captured step reads at every replay."""
+        ctx = _elsewhere(self.m, stream)
+        if ctx is not None:
+            with ctx:
+                return self.step(lr)
+        h = self._hyper
+        lr = self.lr if lr is None else lr
+        h.lr_device = None
+        if isinstance(lr, torch.Tensor):
+            if lr.dtype != torch.float32 or lr.numel() != 1 or lr.device != self.m.device:
+                raise TypeError("lr must be a number or one fp32 on the parameters' device")
+            h.lr_device, lr = lr.data_ptr(), 0.0
+        h.lr, (h.beta1, h.beta2), h.eps, h.weight_decay = lr, self.betas, self.eps, self.weight_decay
+        rc = _load().rehyat_adamw_step(ctypes.byref(self._plan), ctypes.byref(h), _stream_handle(None))
+        if rc != OK:
+            raise RehyatError(rc, "rehyat_adamw_step")
+
+    def moments(self, out=None, stream=None):
+        """(m, v) in fp32, laid out like the buffers of the state: those themselves with 32 bits, with 8 their values in
+        new buffers or in ``out``."""
+        if self.state_bits == 32:
+            return self.m, self.v
+        ctx = _elsewhere(self.m, stream)
+        if ctx is not None:
+            with ctx:
+                return self.moments(out)
+        n = self.m.numel()
+        if out is None:
+            out = [torch.empty(n, device=self.m.device, dtype=torch.float32) for _ in range(2)]
+        for t in out:
+            if t.dtype != torch.float32 or t.device != self.m.device or not t.is_contiguous() or t.numel() != n:
+                raise TypeError("out must be two contiguous CUDA fp32 tensors as long as the state")
+        m, v = out
+        rc = _load().rehyat_adamw_moments(self.m.data_ptr(), self.m_exp.data_ptr(), self.v.data_ptr(),
+                                          self.v_exp.data_ptr(), m.data_ptr(), v.data_ptr(), n, _stream_handle(None))
+        if rc != OK:
+            raise RehyatError(rc, "rehyat_adamw_moments")
+        return m, v
+
+    def load_state(self, m, v, step, m_exp=None, v_exp=None, master=None):
+        """Copies a state in (buffers as in ``m``, ``v``, ``m_exp``, ``v_exp``, ``master``; ``step`` updates made)."""
+        step = int(step)
+        if step < 0:
+            raise ValueError("step must not be negative")
+        given = [(self.m, m), (self.v, v), (self.m_exp, m_exp), (self.v_exp, v_exp)]
+        if master is not None:
+            given.append((self.master, master))
+        for mine, other in given:
+            if (mine is None) != (other is None):
+                raise ValueError("the state is one of other bits")
+            if mine is not None and (mine.shape != other.shape or mine.dtype != other.dtype):
+                raise ValueError("the state has another shape or type")
+        for mine, other in given:
+            if mine is not None:
+                mine.copy_(other)
+        self.step_count.fill_(step)

@@ -7,7 +7,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librehyat.so")
 SOURCES = ["rehyat_api.hip", "rehyat_state.hip", "rehyat_prefix.hip", "rehyat_attn.hip",
-           "rehyat_grad.hip", "rehyat_rope.hip", "rehyat_loss.hip"]
+           "rehyat_grad.hip", "rehyat_rope.hip", "rehyat_loss.hip", "rehyat_adamw.hip"]
 HEADERS = ["rehyat_device.h", "rehyat_kernels.h", "rehyat_state_body.h", "rehyat_host.h", "rehyat_elem.h"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -25,7 +25,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 # slower (the chunk-state kernel) and gradients 0.6 % faster: they keep the default
 EXTRA_FLAGS = {"rehyat_attn.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"],
                # NaN in the inputs is told from numbers there
-               "rehyat_loss.hip": ["-fhonor-nans"]}
+               "rehyat_loss.hip": ["-fhonor-nans"], "rehyat_adamw.hip": ["-fhonor-nans"]}
 
 
 def build_library(force=True, verbose=False):

@@ -140,3 +140,87 @@ def test_distill_loss_binding_rejects_host_tensors():
     y = torch.zeros(1, 2, 8, 64, dtype=torch.bfloat16)
     with pytest.raises(TypeError):
         binding.distill_loss(y, y)
+
+
+# ---- AdamW --------------------------------------------------------------------------------------------------------
+
+
+def adamw_tensors(count=2, **fields):
+    t = (binding.AdamWTensor * count)()
+    for i in range(count):
+        at = A * 0x100 * (i + 1)
+        t[i] = binding.AdamWTensor(at, at + 0x10000, at + 0x20000, at + 0x30000, at + 0x40000, at + 0x50000, at + 0x60000,
+                                   1000, 0, 2)
+    for name, v in fields.items():
+        setattr(t[count - 1], name, v)
+    return t
+
+
+def prepare(t, bits=32, step=0, table=A, bytes_=1 << 20, n=None):
+    plan = binding.AdamWPlan()
+    return binding.library().rehyat_adamw_prepare(t, len(t) if n is None else n, bits, step, table, bytes_,
+                                                  ctypes.byref(plan), None)
+
+
+SECOND = 2 * A * 0x100
+
+
+@pytest.mark.parametrize("bits,bad,code", [
+    (32, dict(param=None), "NULL"), (32, dict(grad=None), "NULL"), (32, dict(m=None), "NULL"), (32, dict(v=None), "NULL"),
+    (8, dict(m_exp=None), "NULL"), (8, dict(v_exp=None), "NULL"), (32, dict(n=-1), "SHAPE"), (32, dict(n=1 << 40), "SHAPE"),
+    (32, dict(param_type=3), "SHAPE"), (32, dict(grad_type=-1), "SHAPE"), (32, dict(param=SECOND + 1), "SHAPE"),
+    (32, dict(grad=SECOND + 0x20002), "SHAPE"), (32, dict(m=SECOND + 0x30008), "SHAPE"), (32, dict(v=SECOND + 0x40004), "SHAPE"),
+    (32, dict(master=SECOND + 0x10002), "SHAPE"),
+    # ranges that overlap: of two tensors, of one, and of the table
+    (32, dict(param=A * 0x100 + 1998), "SHAPE"), (32, dict(m=A * 0x100 + 0x30000 + 3984), "SHAPE"),
+    (32, dict(v=SECOND + 0x30000), "SHAPE"), (32, dict(grad=SECOND + 0x10f9c), "SHAPE"),
+    (8, dict(m_exp=SECOND + 0x3001f), "SHAPE"), (32, dict(param=A + 64), "SHAPE"), (32, dict(n=1 << 39), "WORKSPACE"),
+])
+def test_adamw_prepare_rejects(bits, bad, code):
+    assert prepare(adamw_tensors(**bad), bits) == getattr(binding, "E_" + code)
+
+
+def test_adamw_prepare_rejects_sizes_and_tables():
+    t = adamw_tensors()
+    assert prepare(t, n=0) == prepare(t, bits=16) == prepare(t, step=-1) == binding.E_SHAPE
+    assert prepare(t, table=A + 64) == binding.E_WORKSPACE and prepare(t, table=None) == binding.E_NULL
+    size = binding.library().rehyat_adamw_table_bytes
+    need = size((ctypes.c_int64 * 2)(1000, 1000), 2)
+    assert need % 256 == 0 and prepare(t, bytes_=need - 1) == binding.E_WORKSPACE
+    assert size((ctypes.c_int64 * 1)(-1), 1) == size((ctypes.c_int64 * 1)(1 << 40), 1) == size(None, 1) == 0
+    assert prepare(adamw_tensors(1, n=0)) == binding.E_SHAPE          # nothing to update
+    assert binding.library().rehyat_adamw_prepare(None, 1, 32, 0, A, 1 << 20, None, None) == binding.E_NULL
+
+
+@pytest.mark.parametrize("bad", [
+    dict(lr=-1.0), dict(lr=math.nan), dict(lr=math.inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.5),
+    dict(beta2=math.nan), dict(eps=0.0), dict(eps=-1.0), dict(eps=1e-60), dict(weight_decay=-0.1), dict(lr_device=A + 1),
+])
+def test_adamw_step_rejects(bad):
+    plan = binding.AdamWPlan(A, 5, 2, 32)
+    h = binding.AdamWHyper(1e-3, 0.9, 0.999, 1e-8, 0.01)
+    for name, v in bad.items():
+        setattr(h, name, v)
+    assert binding.library().rehyat_adamw_step(ctypes.byref(plan), ctypes.byref(h), None) == binding.E_SHAPE
+
+
+def test_adamw_step_and_moments_reject_plans_and_pointers():
+    lib = binding.library()
+    h = binding.AdamWHyper(1e-3, 0.9, 0.999, 1e-8, 0.01)
+    P = ctypes.byref
+    assert lib.rehyat_adamw_step(None, P(h), None) == lib.rehyat_adamw_step(P(binding.AdamWPlan(A, 5, 2, 32)), None, None) \
+        == lib.rehyat_adamw_step(P(binding.AdamWPlan()), P(h), None) == binding.E_NULL
+    for plan in ((A, 0, 2, 32), (A, 5, 0, 32), (A, 5, 2, 16)):
+        assert lib.rehyat_adamw_step(P(binding.AdamWPlan(*plan)), P(h), None) == binding.E_SHAPE
+    assert lib.rehyat_adamw_step(P(binding.AdamWPlan(A + 8, 5, 2, 32)), P(h), None) == binding.E_WORKSPACE
+    ok = [A, A, A, A, A, A, 64, None]
+    for i in range(6):
+        assert lib.rehyat_adamw_moments(*ok[:i], None, *ok[i + 1:]) == binding.E_NULL
+    for i in (0, 2, 4, 5):
+        assert lib.rehyat_adamw_moments(*ok[:i], A + 8, *ok[i + 1:]) == binding.E_SHAPE
+    assert lib.rehyat_adamw_moments(*ok[:6], 0, None) == binding.E_SHAPE
+
+
+def test_adamw_binding_rejects_host_tensors():
+    with pytest.raises(TypeError):
+        binding.AdamW([torch.zeros(4)])
