@@ -843,3 +843,56 @@ class AdamW:
             if mine is not None:
                 mine.copy_(other)
         self.step_count.fill_(step)
+
+
+def distill_gradients(q, k, v, y, phi, grads, T, HW, chunk, overlap=0, rope_plan=None, grid=None, start=0,
+                      positions=None, weight=None, scale=None, workspace=None, stream=None):
+    """Loss of one block's distillation (Eq. 19) on one batch, and the gradients of its feature maps, written to
+    ``grads`` (a dict like ``phi``, fp32: an ``AdamW``'s): rotary positions (with a ``rope_plan``; q and k may then have
+    any strides, see ``rope``), the forward pass, ``distill_loss`` against the teacher's output y, ``phi_backward`` on
+    that same forward pass.  Returns the loss, one fp32 on the device."""
+    ctx = _elsewhere(q, stream) if q.is_cuda else None
+    if ctx is not None:
+        with ctx:
+            return distill_gradients(q, k, v, y, phi, grads, T, HW, chunk, overlap, rope_plan, grid, start, positions,
+                                     weight, scale, workspace)
+    if rope_plan is None and (grid is not None or start != 0 or positions is not None):
+        raise ValueError("positions need a rope_plan")
+    if rope_plan is not None:
+        if grid is not None and len(grid) == 2 and grid[0] * grid[1] != HW:
+            raise ValueError("the grid's rows and columns do not make a frame of HW tokens")
+        q, k = rope(q, k, rope_plan, grid=grid, start=start, positions=positions)
+    _check_qkv(q, k, v)
+    B, H, N, d = q.shape
+    if N != T * HW:
+        raise ValueError("N != T*HW")
+    p, Hp = _phi_struct(phi, d)
+    if Hp != H:
+        raise ValueError("phi head count differs from q")
+    out = torch.empty_like(q)
+    nS, nL = (torch.empty(B, H, N, device=q.device, dtype=torch.float32) for _ in range(2))
+    kept = DebugOut(nS=nS.data_ptr(), nL=nL.data_ptr())
+    rc = _load().rehyat_forward_ex(q.data_ptr(), k.data_ptr(), v.data_ptr(), ctypes.byref(p), out.data_ptr(), B, H, T,
+                                   HW, d, chunk, overlap, 1, STAB_ROWMAX, ctypes.byref(kept), _stream_handle(None))
+    if rc != OK:
+        raise RehyatError(rc, "rehyat_forward_ex")
+    loss, g = distill_loss(out, y, scale=scale, weight=weight)
+    phi_backward(q, k, v, phi, g, T, HW, chunk, overlap=overlap, workspace=workspace, grads=grads, saved=(out, nS, nL))
+    return loss
+
+
+def distill_step(q, k, v, y, phi, opt, T, HW, chunk, lr=None, stream=None, **kw):
+    """One step of the distillation of one block: ``distill_gradients`` (which see for the other arguments), then
+    phi <- AdamW(phi).  ``opt`` is an ``AdamW`` over ``phi``, a dict.  (Several blocks share one optimiser, and one
+    launch, with AdamW([phi_0, phi_1, ...]), a ``distill_gradients`` into ``opt.grads[i]`` each, and ``opt.step()``.)
+    Returns the loss before the update."""
+    if not isinstance(opt.grads, dict) or opt.grads.keys() != phi.keys() or \
+            any(a is not b for a, b in zip(opt.params, phi.values())):
+        raise ValueError("opt must be an AdamW over this phi")
+    ctx = _elsewhere(q, stream) if q.is_cuda else None
+    if ctx is not None:
+        with ctx:
+            return distill_step(q, k, v, y, phi, opt, T, HW, chunk, lr, **kw)
+    loss = distill_gradients(q, k, v, y, phi, opt.grads, T, HW, chunk, **kw)
+    opt.step(lr=lr)
+    return loss
