@@ -459,7 +459,7 @@ int rehyat_distill_loss(const void *y_hat, const void *y, int type,
  * with every replay.
  * rehyat_adamw_step: one update of all tensors.  lr_device (DEVICE fp32, nullable)
  * replaces lr, for schedules under replay.  Steps of one table must be ordered.
- * rehyat_adamw_moments: the values of 8-bit moments of n elements (DEVICE fp32 out,
+ * rehyat_adamw_moments: the values of n 8-bit moments, m and v in whole groups as above (DEVICE fp32 out,
  * 16-byte aligned).
  * Errors: REHYAT_E_NULL, REHYAT_E_SHAPE (also: overlapping ranges; lr, eps or
  * weight_decay negative or not finite, eps 0, a beta outside [0, 1)), REHYAT_E_WORKSPACE.

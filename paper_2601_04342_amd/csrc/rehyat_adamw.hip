@@ -2,7 +2,7 @@
 //
 // Bound by HBM: gradient, weight and both moments are read once, weight and moments written once; some thirty flops an
 // element stand against 18 (moments in 8 bits) to 30 bytes.  A table in device memory, written when the tensors are
-// named, cuts all of them into items of 4,096 elements, so that one launch serves any number of tensors of any size
+// named, cuts all of them into items of 1,024 elements, so that one launch serves any number of tensors of any size
 // without the host touching them again.
 //
 // Moments in 8 bits: groups of 32 elements share an exponent, a power of two, so scaling is exact and every rounding is
@@ -22,17 +22,24 @@ namespace rehyat {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kItem = 4096;    // elements of an item: a multiple of the group
+constexpr int kItem = 4 * kThreads;    // elements of an item: four a thread
 constexpr int kGroup = 32;
 
+// Workgroups of a step say that they have read `step`, each to one of kCounters counters in a cache line of its own, and
+// the last of each to `arrived`: atomics on one address are done one after the other, 45 ns each, and the step of one
+// block's eight tensors (71 MB, 2,048 workgroups) took 97 us with all of them on one counter, at its end; now 14 us.
+constexpr int kCounters = 64;
 struct Header {
   int64_t step;      // updates made (the caller may see and set it)
-  uint32_t arrived;  // workgroups of the running step that are done
+  uint32_t arrived;  // counters that are full
   uint32_t n_tensors;
   int64_t items;
-  int64_t pad[5];
+  int64_t pad[13];
+  struct {
+    uint32_t arrived, pad[31];
+  } counter[kCounters];
 };
-static_assert(sizeof(Header) == 64, "the tensors' descriptions follow at 64 bytes");
+static_assert(sizeof(Header) == 128 * (1 + kCounters), "lines of 128 bytes; the tensors' descriptions follow");
 
 struct Desc {
   void* param;
@@ -52,9 +59,9 @@ __host__ __device__ inline size_t map_offset(int n_tensors) { return sizeof(Head
 constexpr int kPrepare = 40;   // descriptions a launch carries in its arguments (3.3 KB of them)
 struct PrepareArgs {
   Desc desc[kPrepare];
-  Header header;
   char* table;
-  int first, count;
+  int64_t step, items;
+  int first, count, n_tensors;
 };
 
 __global__ __launch_bounds__(kThreads) void adamw_prepare_kernel(PrepareArgs a) {
@@ -62,15 +69,26 @@ __global__ __launch_bounds__(kThreads) void adamw_prepare_kernel(PrepareArgs a) 
   const int i = a.first + blockIdx.x;
   if (threadIdx.x == 0) {
     ((Desc*)(a.table + sizeof(Header)))[i] = d;
-    if (i == 0) *(Header*)a.table = a.header;
   }
-  int32_t* map = (int32_t*)(a.table + map_offset(a.header.n_tensors)) + d.first_item;
+  if (i == 0) {
+    Header* const h = (Header*)a.table;
+    if (threadIdx.x == 0) {
+      h->step = a.step;
+      h->arrived = 0;
+      h->n_tensors = (uint32_t)a.n_tensors;
+      h->items = a.items;
+    }
+    for (int k = threadIdx.x; k < kCounters; k += kThreads) h->counter[k].arrived = 0;
+  }
+  int32_t* map = (int32_t*)(a.table + map_offset(a.n_tensors)) + d.first_item;
   const int64_t items = (d.n + kItem - 1) / kItem;
   for (int64_t k = threadIdx.x; k < items; k += kThreads) map[k] = i;
 }
 
 // ---- 8-bit moments ------------------------------------------------------------------------------------------------
 
+// (of a value, not of a vector's element in place: this compiler's bit cast of one takes the vector's first)
+__device__ __forceinline__ uint32_t bits_of(float x) { return __builtin_bit_cast(uint32_t, x); }
 __device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (uint32_t)e << 23); }   // 2^(e - 127)
 
 // exponent of a group whose largest magnitude has the bits `top`; `least` keeps factors and codes in range
@@ -80,32 +98,101 @@ __device__ __forceinline__ int group_exponent(uint32_t top, int least) {
 }
 constexpr int kLeastM = 8, kLeastV = 31;
 
-__device__ __forceinline__ float decode_m(uint32_t code, int e) {
-  if (e == 255) return __builtin_nanf("");
-  return __builtin_amdgcn_cvt_f32_fp8((int)code, 0) * power_of_two((e < kLeastM ? kLeastM : e) - 7);
+// four codes of one group at a time, as they stand in a word
+__device__ __forceinline__ f32x4 decode_m(uint32_t codes, int e) {
+  const float f = power_of_two((e < kLeastM ? kLeastM : e) - 7);
+  const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+  const f32x4 x = {lo[0] * f, lo[1] * f, hi[0] * f, hi[1] * f};
+  const float nan = __builtin_nanf("");
+  return e == 255 ? f32x4{nan, nan, nan, nan} : x;
 }
-__device__ __forceinline__ uint32_t encode_m(float m, int e) {
-  if (e == 255) return 0;
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(m * power_of_two(261 - e), 0.f, 0, false) & 255;
+__device__ __forceinline__ uint32_t encode_m(f32x4 m, int e) {
+  const float f = power_of_two(261 - e);
+  int codes = __builtin_amdgcn_cvt_pk_fp8_f32(m[0] * f, m[1] * f, 0, false);
+  codes = __builtin_amdgcn_cvt_pk_fp8_f32(m[2] * f, m[3] * f, codes, true);
+  return e == 255 ? 0u : (uint32_t)codes;
 }
-__device__ __forceinline__ float decode_v(uint32_t code, int e) {
-  if (e == 255) return __builtin_nanf("");
-  return code == 0 ? 0.f : __builtin_bit_cast(float, (code + ((uint32_t)((e < kLeastV ? kLeastV : e) - 30) << 3)) << 20);
+__device__ __forceinline__ f32x4 decode_v(uint32_t codes, int e) {
+  const uint32_t least = (uint32_t)((e < kLeastV ? kLeastV : e) - 30) << 3;
+  f32x4 x;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t c = codes >> (8 * k) & 255;
+    x[k] = e == 255 ? __builtin_nanf("") : c == 0 ? 0.f : __builtin_bit_cast(float, (c + least) << 20);
+  }
+  return x;
 }
-__device__ __forceinline__ uint32_t encode_v(float v, int e) {
-  const uint32_t bits = __builtin_bit_cast(uint32_t, v);
-  if (e == 255 || bits == 0) return 0;
-  const int code = (int)((bits + 0x7ffffu + ((bits >> 20) & 1)) >> 20) - ((e - 30) << 3);
-  return code < 1 ? 1 : code > 255 ? 255 : code;
+__device__ __forceinline__ uint32_t encode_v(f32x4 v, int e) {
+  uint32_t codes = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t bits = bits_of(v[k]);
+    int c = (int)((bits + 0x7ffffu + ((bits >> 20) & 1)) >> 20) - ((e - 30) << 3);
+    c = c < 1 ? 1 : c > 255 ? 255 : c;
+    codes |= (bits == 0 ? 0u : (uint32_t)c) << (8 * k);
+  }
+  return e == 255 ? 0u : codes;
+}
+// largest over the eight lanes that hold a group: neighbours, pairs, then the two halves mirrored
+__device__ __forceinline__ uint32_t group_max(uint32_t x) {
+  auto other = [](uint32_t y, auto ctrl) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)y, decltype(ctrl)::value, 0xf, 0xf, true);
+  };
+  uint32_t y = other(x, std::integral_constant<int, 0xb1>{});    // quad_perm 1 0 3 2
+  x = y > x ? y : x;
+  y = other(x, std::integral_constant<int, 0x4e>{});             // quad_perm 2 3 0 1
+  x = y > x ? y : x;
+  y = other(x, std::integral_constant<int, 0x141>{});            // lanes 0 .. 7 reversed
+  return y > x ? y : x;
 }
 
-__device__ __forceinline__ float load(int type, const void* p, int64_t i) {
-  return type == REHYAT_FP32 ? ((const float*)p)[i]
-         : type == REHYAT_BF16 ? Bf16::get(((const uint16_t*)p)[i]) : Fp16::get(((const uint16_t*)p)[i]);
+// Four elements from i on; a caller's tensor may begin at any element, and end inside the four (`left` of them are there).
+// The pointers come out of the table, where the compiler cannot see that they are to global memory.
+typedef f32x4 f32x4_e __attribute__((aligned(4)));
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+typedef u16x4 u16x4_e __attribute__((aligned(2)));
+template <typename T>
+using global = __attribute__((address_space(1))) T;
+template <typename T>
+__device__ __forceinline__ global<T>* at(const void* p, int64_t i) { return (global<T>*)(T*)p + i; }
+template <typename E, typename V>
+__device__ __forceinline__ f32x4 load4(const void* p, int64_t i, int left) {
+  const global<typename E::store>* const q = at<typename E::store>(p, i);
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  if (left >= 4) {
+    const V y = *(const global<V>*)q;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = E::get(y[k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (k < left) x[k] = E::get(q[k]);
+  }
+  return x;
 }
-__device__ __forceinline__ void store(int type, void* p, int64_t i, float x) {
-  if (type == REHYAT_FP32) ((float*)p)[i] = x;
-  else ((uint16_t*)p)[i] = type == REHYAT_BF16 ? Bf16::put(x) : Fp16::put(x);
+template <typename E, typename V>
+__device__ __forceinline__ void store4(void* p, int64_t i, int left, f32x4 x) {
+  global<typename E::store>* const q = at<typename E::store>(p, i);
+  if (left >= 4) {
+    V y;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = E::put(x[k]);
+    *(global<V>*)q = y;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (k < left) q[k] = E::put(x[k]);
+  }
+}
+__device__ __forceinline__ f32x4 load(int type, const void* p, int64_t i, int left) {
+  if (type == REHYAT_FP32) return load4<Fp32, f32x4_e>(p, i, left);
+  if (type == REHYAT_BF16) return load4<Bf16, u16x4_e>(p, i, left);
+  return load4<Fp16, u16x4_e>(p, i, left);
+}
+__device__ __forceinline__ void store(int type, void* p, int64_t i, int left, f32x4 x) {
+  if (type == REHYAT_FP32) store4<Fp32, f32x4_e>(p, i, left, x);
+  else if (type == REHYAT_BF16) store4<Bf16, u16x4_e>(p, i, left, x);
+  else store4<Fp16, u16x4_e>(p, i, left, x);
 }
 
 // ---- the step -----------------------------------------------------------------------------------------------------
@@ -117,88 +204,126 @@ struct StepArgs {
   float beta1, rest1, beta2, rest2, eps;   // rest = 1 - beta
 };
 
+// What a thread holds of an item: four elements.
+template <int BITS>
+struct Quad {
+  f32x4 g, p;
+  f32x4 m, v;            // 32 bits
+  uint32_t cm, cv;       // 8 bits: codes, and the group's exponents
+  int em, ev;
+};
+
 template <int BITS>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a) {
   Header* const header = (Header*)a.table;
   const Desc* const descs = (const Desc*)(a.table + sizeof(Header));
-  const int32_t* const map = (const int32_t*)(a.table + map_offset(header->n_tensors));
-  const int64_t step = header->step + 1;
-  const double lr = a.lr_device ? (double)*a.lr_device : a.lr;
-  // 1 - beta^t, with log(beta) from the host
-  const float rate = (float)(lr / -expm1((double)step * a.log_beta1));
-  const float root = (float)(1.0 / sqrt(-expm1((double)step * a.log_beta2)));
-  const float keep = (float)(1.0 - lr * a.weight_decay);
-  for (int64_t item = blockIdx.x; item < header->items; item += gridDim.x) {
-    const Desc d = descs[map[item]];
-    const int64_t base = (item - d.first_item) * kItem;
-    for (int k = threadIdx.x; k < kItem; k += kThreads) {
-      const int64_t i = base + k;
-      const bool in = i < d.n;
-      float g = 0.f, m = 0.f, v = 0.f, p = 0.f;
-      if (in) {
-        g = load(d.grad_type, d.grad, i);
-        p = d.master ? d.master[i] : load(d.param_type, d.param, i);
-      }
-      if (BITS == 32) {
-        if (in) {
-          m = ((const float*)d.m)[i];
-          v = ((const float*)d.v)[i];
-        }
-        m = a.beta1 * m + a.rest1 * g;
-        v = a.beta2 * v + a.rest2 * (g * g);
-        if (in) {
-          ((float*)d.m)[i] = m;
-          ((float*)d.v)[i] = v;
-        }
-      } else {
-        if (in) {
-          m = decode_m(((const uint8_t*)d.m)[i], d.m_exp[i / kGroup]);
-          v = decode_v(((const uint8_t*)d.v)[i], d.v_exp[i / kGroup]);
-        }
-        // in 64 bits, where products of 24-bit numbers are exact: m, v are the true sums rounded once, so that what
-        // lies half way between two codes is decided by the numbers and not by how they were added
-        m = (float)fma((double)a.beta1, (double)m, (double)a.rest1 * (double)g);
-        v = (float)fma((double)a.beta2, (double)v, (double)a.rest2 * ((double)g * (double)g));
-        uint32_t top_m = __builtin_bit_cast(uint32_t, m) & 0x7fffffffu, top_v = __builtin_bit_cast(uint32_t, v) & 0x7fffffffu;
+  const int32_t* const map = (const int32_t*)(a.table + map_offset((int)header->n_tensors));
+  const int64_t items = header->items;
+  Desc d;
+  int64_t i;       // the thread's first element; `left` of its four are there
+  int left;
+  bool active;     // 8 bits: the lanes of a group stay together, whose codes reach to its end
+  Quad<BITS> x;
+  auto fetch = [&](int64_t item) {
+    d = descs[map[item]];
+    i = (item - d.first_item) * kItem + 4 * threadIdx.x;
+    left = d.n - i < 4 ? (int)(d.n - i) : 4;
+    active = BITS == 32 ? left > 0 : i / kGroup * kGroup < d.n;
+    if (!active) return;
+    x.g = load(d.grad_type, d.grad, i, left);
+    x.p = d.master ? load4<Fp32, f32x4_e>(d.master, i, left) : load(d.param_type, d.param, i, left);
+    if (BITS == 32) {
+      x.m = load4<Fp32, f32x4>(d.m, i, left);
+      x.v = load4<Fp32, f32x4>(d.v, i, left);
+    } else {
+      x.cm = *at<uint32_t>(d.m, i / 4);
+      x.cv = *at<uint32_t>(d.v, i / 4);
+      x.em = *at<uint8_t>(d.m_exp, i / kGroup);
+      x.ev = *at<uint8_t>(d.v_exp, i / kGroup);
+    }
+  };
+  fetch(blockIdx.x);
+
+  // factors of this update, and the workgroup's arrival (its answer is not looked at before the end)
+  __shared__ float factors[3];
+  int64_t step = 0;
+  uint32_t before = 0;
+  const uint32_t counters = gridDim.x < kCounters ? gridDim.x : kCounters, mine = blockIdx.x % counters;
+  if (threadIdx.x == 0) {
+    step = header->step + 1;
+    const double lr = a.lr_device ? (double)*a.lr_device : a.lr;
+    // 1 - beta^t, with log(beta) from the host
+    factors[0] = (float)(lr / -expm1((double)step * a.log_beta1));
+    factors[1] = (float)(1.0 / sqrt(-expm1((double)step * a.log_beta2)));
+    factors[2] = (float)(1.0 - lr * a.weight_decay);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0)
+    before = __hip_atomic_fetch_add(&header->counter[mine].arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const float rate = factors[0], root = factors[1], keep = factors[2];
+
+  for (int64_t item = blockIdx.x; item < items; ) {
+    const Desc e = d;
+    const Quad<BITS> y = x;
+    const int64_t j = i;
+    const int there = left;
+    const bool on = active;
+    item += gridDim.x;
+    if (item < items) fetch(item);   // in flight behind what follows
+    if (!on) continue;
+    f32x4 m, v, p = y.p;
+    if (BITS == 32) {
+      m = a.beta1 * y.m + a.rest1 * y.g;
+      v = a.beta2 * y.v + a.rest2 * (y.g * y.g);
+      store4<Fp32, f32x4>(e.m, j, there, m);
+      store4<Fp32, f32x4>(e.v, j, there, v);
+    } else {
+      m = decode_m(y.cm, y.em);
+      v = decode_v(y.cv, y.ev);
+      // in 64 bits, where products of 24-bit numbers are exact: m, v are the true sums rounded once, so that what
+      // lies half way between two codes is decided by the numbers and not by how they were added
+      uint32_t top_m = 0, top_v = 0;
 #pragma unroll
-        for (int x = 16; x; x >>= 1) {
-          const uint32_t om = __shfl_xor(top_m, x), ov = __shfl_xor(top_v, x);
-          top_m = om > top_m ? om : top_m;
-          top_v = ov > top_v ? ov : top_v;
-        }
-        const int em = group_exponent(top_m, kLeastM), ev = group_exponent(top_v, kLeastV);
-        if (i < (d.n + kGroup - 1) / kGroup * kGroup) {
-          ((uint8_t*)d.m)[i] = encode_m(m, em);
-          ((uint8_t*)d.v)[i] = encode_v(v, ev);
-          if (i % kGroup == 0) {
-            d.m_exp[i / kGroup] = em;
-            d.v_exp[i / kGroup] = ev;
-          }
-        }
+      for (int k = 0; k < 4; ++k) {
+        m[k] = (float)fma((double)a.beta1, (double)m[k], (double)a.rest1 * (double)y.g[k]);
+        v[k] = (float)fma((double)a.beta2, (double)v[k], (double)a.rest2 * ((double)y.g[k] * (double)y.g[k]));
+        if (k >= there) m[k] = v[k] = 0.f;
+        const uint32_t bm = bits_of(m[k]) & 0x7fffffffu, bv = bits_of(v[k]) & 0x7fffffffu;
+        top_m = bm > top_m ? bm : top_m;
+        top_v = bv > top_v ? bv : top_v;
       }
-      p = p * keep - rate * (m / (sqrtf(v) * root + a.eps));
-      if (in) {
-        if (d.master) d.master[i] = p;
-        store(d.param_type, d.param, i, p);
+      const int em = group_exponent(group_max(top_m), kLeastM), ev = group_exponent(group_max(top_v), kLeastV);
+      *at<uint32_t>(e.m, j / 4) = encode_m(m, em);
+      *at<uint32_t>(e.v, j / 4) = encode_v(v, ev);
+      if (threadIdx.x % (kGroup / 4) == 0) {
+        *at<uint8_t>(e.m_exp, j / kGroup) = em;
+        *at<uint8_t>(e.v_exp, j / kGroup) = ev;
       }
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) p[k] = p[k] * keep - rate * (m[k] / (sqrtf(v[k]) * root + a.eps));
+    if (e.master) store4<Fp32, f32x4_e>(e.master, j, there, p);
+    store(e.param_type, e.param, j, there, p);
   }
-  // the last workgroup counts the update: by then every workgroup has read the count
-  __syncthreads();
-  if (threadIdx.x == 0 &&
-      __hip_atomic_fetch_add(&header->arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1) {
-    header->arrived = 0;
-    header->step = step;
+
+  // the last to have read the count writes the next one
+  if (threadIdx.x == 0 && before == (gridDim.x - mine + counters - 1) / counters - 1 &&
+      __hip_atomic_fetch_add(&header->arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == counters - 1) {
+    for (uint32_t k = 0; k < counters; ++k)
+      __hip_atomic_store(&header->counter[k].arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(&header->arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(&header->step, step, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
 }
 
 __global__ __launch_bounds__(kThreads) void adamw_moments_kernel(const uint8_t* m, const uint8_t* m_exp, const uint8_t* v,
                                                                  const uint8_t* v_exp, float* m_out, float* v_out,
                                                                  int64_t n) {
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t i = 4 * ((int64_t)blockIdx.x * kThreads + threadIdx.x);
   if (i >= n) return;
-  m_out[i] = decode_m(m[i], m_exp[i / kGroup]);
-  v_out[i] = decode_v(v[i], v_exp[i / kGroup]);
+  const int left = n - i < 4 ? (int)(n - i) : 4;
+  store4<Fp32, f32x4>(m_out, i, left, decode_m(*(const uint32_t*)(m + i), m_exp[i / kGroup]));
+  store4<Fp32, f32x4>(v_out, i, left, decode_v(*(const uint32_t*)(v + i), v_exp[i / kGroup]));
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------
@@ -288,9 +413,9 @@ int rehyat_adamw_prepare(const rehyat_adamw_tensor* tensors, int n_tensors, int 
   if (rc != REHYAT_OK) return rc;
 
   PrepareArgs a{};
-  a.header.step = step;
-  a.header.n_tensors = (uint32_t)n_tensors;
-  a.header.items = items;
+  a.step = step;
+  a.n_tensors = n_tensors;
+  a.items = items;
   a.table = (char*)table;
   int64_t at = 0;
   for (int first = 0; first < n_tensors; first += kPrepare) {
@@ -346,7 +471,7 @@ int rehyat_adamw_moments(const void* m, const void* m_exp, const void* v, const 
   if (!m || !m_exp || !v || !v_exp || !m_out || !v_out) return REHYAT_E_NULL;
   if (n < 1 || n >= ((int64_t)1 << 38)) return REHYAT_E_SHAPE;
   if (!aligned16(m) || !aligned16(v) || !aligned16(m_out) || !aligned16(v_out)) return REHYAT_E_SHAPE;
-  adamw_moments_kernel<<<(unsigned)((n + kThreads - 1) / kThreads), kThreads, 0, (hipStream_t)stream>>>(
+  adamw_moments_kernel<<<(unsigned)((n + 4 * kThreads - 1) / (4 * kThreads)), kThreads, 0, (hipStream_t)stream>>>(
       (const uint8_t*)m, (const uint8_t*)m_exp, (const uint8_t*)v, (const uint8_t*)v_exp, m_out, v_out, n);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "AdamW moments kernel launch");
