@@ -462,7 +462,7 @@ int rehyat_distill_loss(const void *y_hat, const void *y, int type,
  * rehyat_adamw_moments: the values of n 8-bit moments, m and v in whole groups as above (DEVICE fp32 out,
  * 16-byte aligned).
  * Errors: REHYAT_E_NULL, REHYAT_E_SHAPE (also: overlapping ranges; lr, eps or
- * weight_decay negative or not finite, eps 0, a beta outside [0, 1)), REHYAT_E_WORKSPACE.
+ * weight_decay negative or not finite, eps below FLT_MIN, a beta outside [0, 1)), REHYAT_E_WORKSPACE.
  */
 typedef struct {
   void *param;
