@@ -335,7 +335,7 @@ int rehyat_step(const void *q_t, const void *k_win, const void *v_win,
  *
  * rehyat_rope_plan (HOST struct)
  *   turns     DEVICE, rot / 2 values of rehyat_rope_turns
- *   d, rot    head width (2 .. 512) and rotated part of it (even, 2 .. d)
+ *   d, rot    head width (even, 2 .. 512) and rotated part of it (even, 2 .. d)
  *   layout    REHYAT_ROPE_INTERLEAVED: pair i is elements 2i, 2i+1;
  *             REHYAT_ROPE_HALF: elements i, i + rot/2
  *   axes      1 .. 3; section[x] pairs in a row belong to axis x (each >= 1, they

@@ -501,8 +501,8 @@ class Rope:
     def __init__(self, d, rot=None, layout="interleaved", base=10000.0, sections=None, scaling=None, freqs=None,
                  scale=None, device="cuda"):
         rot = d if rot is None else rot
-        if not 2 <= rot <= d <= 512 or rot % 2:
-            raise ValueError("rot must be even, 2 <= rot <= d <= 512")
+        if not 2 <= rot <= d <= 512 or rot % 2 or d % 2:
+            raise ValueError("rot and d must be even, 2 <= rot <= d <= 512")
         sections = (rot // 2,) if sections is None else tuple(int(n) for n in sections)
         if not 1 <= len(sections) <= 3 or min(sections) < 1 or sum(sections) != rot // 2:
             raise ValueError("sections must be one to three positive counts of pairs that add up to rot / 2")

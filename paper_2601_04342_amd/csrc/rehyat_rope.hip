@@ -15,6 +15,8 @@
 namespace rehyat {
 namespace {
 
+constexpr int kMostHeads = 16, kWaves = 4096;
+
 struct RopeOperand {
   const void* x;
   void* out;
@@ -33,7 +35,7 @@ struct RopeArgs {
   int pos_bits;
   uint32_t items, slots;         // B * N * slots; pieces of a row
   uint32_t N, frame, cols;       // frame: tokens of one step of the first axis
-  int rot, axes, sec1, sec2;     // pairs from sec1 on belong to axis 1, from sec2 on to axis 2
+  int d, rot, axes, sec1, sec2;  // pairs from sec1 on belong to axis 1, from sec2 on to axis 2
   uint32_t copies_from;          // slots from here on copy
   float scale, sign;
 };
@@ -51,9 +53,42 @@ __device__ __forceinline__ void cos_sin(uint32_t t, float* c, float* s) {
   *s = quarter >= 2 ? -b : b;
 }
 
-template <typename E, int LAYOUT>
+// V elements of a row that stand together, loaded and stored as one; rows begin at any element.
+template <typename E, int V>
+struct Vec {
+  typedef typename E::store raw __attribute__((ext_vector_type(V), aligned(sizeof(typename E::store))));
+  static __device__ __forceinline__ raw load(const typename E::store* p) { return *(const raw*)p; }
+  static __device__ __forceinline__ void store(typename E::store* p, raw x) { *(raw*)p = x; }
+  static __device__ __forceinline__ float get(raw x, int i) { return E::get(x[i]); }
+};
+template <typename E>
+struct Vec<E, 1> {
+  typedef typename E::store raw;
+  static __device__ __forceinline__ raw load(const raw* p) { return *p; }
+  static __device__ __forceinline__ void store(raw* p, raw x) { *p = x; }
+  static __device__ __forceinline__ float get(raw x, int) { return E::get(x); }
+};
+template <typename E, int V>
+__device__ __forceinline__ typename Vec<E, V>::raw round_all(const float* x) {
+  typename Vec<E, V>::raw r;
+  if constexpr (V == 1) {
+    r = E::put(x[0]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) r[i] = E::put(x[i]);
+  }
+  return r;
+}
+
+// A thread holds V pairs' worth of a row: with the half layout V elements of either half, otherwise V elements in a row.
+// Beyond the rotated part it holds as many elements, which it copies: `keep`.
+template <typename E, int LAYOUT, int V>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   typedef typename E::store T;
+  typedef Vec<E, V> W;
+  typedef typename W::raw R;
+  constexpr bool kHalf = LAYOUT == REHYAT_ROPE_HALF;
+  constexpr int kPairs = kHalf ? V : V / 2;
   const uint32_t i = blockIdx.x * 256 + threadIdx.x;
   if (i >= a.items) return;
   const uint32_t token = i / a.slots, slot = i - token * a.slots;
@@ -62,42 +97,86 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   const RopeOperand& op = second ? a.op[1] : a.op[0];
   const int h0 = ((int)blockIdx.y - (second ? a.groups0 : 0)) * a.group;
   const int h1 = h0 + a.group < op.heads ? h0 + a.group : op.heads;
-  const T* x = (const T*)op.x + b * op.xb + n * op.xn + h0 * op.xh;
-  T* out = (T*)op.out + b * op.ob + n * op.on + h0 * op.oh;
 
-  if (slot >= a.copies_from) {
-    const uint32_t col = a.rot + slot - a.copies_from;
-    for (int h = h0; h < h1; ++h, x += op.xh, out += op.oh) out[col] = x[col];
-    return;
-  }
-  const int pair = slot, axis = pair >= a.sec2 ? 2 : pair >= a.sec1 ? 1 : 0;
-  uint64_t pos;   // modulo 2^64
-  if (a.pos) {
-    const int64_t at = b * a.pos_b + n * a.pos_n + axis;
-    pos = a.pos_bits == 64 ? ((const int64_t*)a.pos)[at] : (int64_t)((const int32_t*)a.pos)[at];
+  const bool keep = slot >= a.copies_from;
+  uint32_t first, other = 0;
+  if (kHalf) {
+    first = keep ? a.rot + 2 * V * (slot - a.copies_from) : V * slot;
+    other = keep ? first + V : first + a.rot / 2;
+    if (other >= (uint32_t)a.d) other = first;   // an odd number of copied pieces: the last twice
   } else {
-    const uint32_t f = n / a.frame, r = n - f * a.frame;
-    pos = axis == 0 ? a.start + f : axis == a.axes - 1 ? r % a.cols : r / a.cols;
+    first = V * slot;
   }
-  float c, s;
-  cos_sin((uint32_t)((pos * a.turns[pair]) >> 32), &c, &s);
-  c *= a.scale;
-  s *= a.scale * a.sign;
-  const uint32_t first = LAYOUT == REHYAT_ROPE_INTERLEAVED ? 2 * slot : slot;
-  const uint32_t other = LAYOUT == REHYAT_ROPE_INTERLEAVED ? first + 1 : first + a.rot / 2;
-  for (int h = h0; h < h1; ++h, x += op.xh, out += op.oh) {
-    const float u = E::get(x[first]), v = E::get(x[other]);
-    out[first] = E::put(u * c - v * s);
-    out[other] = E::put(v * c + u * s);
+  const T* x = (const T*)op.x + b * op.xb + n * op.xn + h0 * op.xh + first;
+  T* out = (T*)op.out + b * op.ob + n * op.on + h0 * op.oh + first;
+  const int64_t to_other = (int64_t)other - first;
+
+  float c[kPairs], s[kPairs];
+  if (!keep) {
+    uint64_t pos[3];   // modulo 2^64
+    if (a.pos) {
+      const int64_t at = b * a.pos_b + n * a.pos_n;
+#pragma unroll
+      for (int x = 0; x < 3; ++x)
+        if (x < a.axes) pos[x] = a.pos_bits == 64 ? ((const int64_t*)a.pos)[at + x] : (int64_t)((const int32_t*)a.pos)[at + x];
+    } else {
+      const uint32_t f = n / a.frame, r = n - f * a.frame, y = r / a.cols;
+      pos[0] = a.start + f;
+      pos[1] = a.axes == 2 ? r : y;
+      pos[2] = r - y * a.cols;
+    }
+    const uint32_t pair0 = kPairs * slot;
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) {
+      const int pair = pair0 + k;
+      const uint64_t p = pair >= a.sec2 ? pos[2] : pair >= a.sec1 ? pos[1] : pos[0];
+      cos_sin((uint32_t)((p * a.turns[pair]) >> 32), &c[k], &s[k]);
+      c[k] *= a.scale;
+      s[k] *= a.scale * a.sign;
+    }
+  }
+  constexpr int kDepth = 4;   // heads in flight
+  for (int h = h0; h < h1; h += kDepth, x += kDepth * op.xh, out += kDepth * op.oh) {
+    R u[kDepth], v[kDepth];
+#pragma unroll
+    for (int k = 0; k < kDepth; ++k)
+      if (h + k < h1) {
+        u[k] = W::load(x + k * op.xh);
+        if (kHalf) v[k] = W::load(x + k * op.xh + to_other);
+      }
+#pragma unroll
+    for (int k = 0; k < kDepth; ++k)
+      if (h + k < h1) {
+        if (!keep) {
+          float lo[V], hi[V];
+#pragma unroll
+          for (int j = 0; j < kPairs; ++j) {
+            const float p = kHalf ? W::get(u[k], j) : W::get(u[k], 2 * j), q = kHalf ? W::get(v[k], j) : W::get(u[k], 2 * j + 1);
+            const float rp = p * c[j] - q * s[j], rq = q * c[j] + p * s[j];
+            if (kHalf) lo[j] = rp, hi[j] = rq;
+            else lo[2 * j] = rp, lo[2 * j + 1] = rq;
+          }
+          u[k] = round_all<E, V>(lo);
+          if (kHalf) v[k] = round_all<E, V>(hi);
+        }
+        W::store(out + k * op.oh, u[k]);
+        if (kHalf) W::store(out + k * op.oh + to_other, v[k]);
+      }
   }
 }
 
-template <typename E>
+template <typename E, int V>
 void launch(const RopeArgs& a, int layout, dim3 grid, hipStream_t st) {
   if (layout == REHYAT_ROPE_INTERLEAVED)
-    rope_kernel<E, REHYAT_ROPE_INTERLEAVED><<<grid, 256, 0, st>>>(a);
+    rope_kernel<E, REHYAT_ROPE_INTERLEAVED, (V < 2 ? 2 : V)><<<grid, 256, 0, st>>>(a);
   else
-    rope_kernel<E, REHYAT_ROPE_HALF><<<grid, 256, 0, st>>>(a);
+    rope_kernel<E, REHYAT_ROPE_HALF, V><<<grid, 256, 0, st>>>(a);
+}
+template <typename E>
+void launch(const RopeArgs& a, int layout, int v, dim3 grid, hipStream_t st) {
+  if (v == 16 / sizeof(typename E::store)) launch<E, 16 / sizeof(typename E::store)>(a, layout, grid, st);
+  else if (v == 2) launch<E, 2>(a, layout, grid, st);
+  else launch<E, 1>(a, layout, grid, st);
 }
 
 // Whether the rows of an output with these strides are apart: every dimension steps over all that the smaller ones span.
@@ -146,7 +225,7 @@ int rehyat_rope(const rehyat_rope_operand* operands, int n_operands, const rehya
   if (n_operands < 1 || n_operands > 2 || B < 1 || N < 1 || !valid_type(type)) return REHYAT_E_SHAPE;
   if (inverse != 0 && inverse != 1) return REHYAT_E_SHAPE;
   const int d = plan->d, rot = plan->rot, axes = plan->axes;
-  if (d < 2 || d > 512 || rot < 2 || rot > d || rot % 2) return REHYAT_E_SHAPE;
+  if (d < 2 || d > 512 || d % 2 || rot < 2 || rot > d || rot % 2) return REHYAT_E_SHAPE;
   if (plan->layout != REHYAT_ROPE_INTERLEAVED && plan->layout != REHYAT_ROPE_HALF) return REHYAT_E_SHAPE;
   if (axes < 1 || axes > 3 || !std::isfinite(plan->scale)) return REHYAT_E_SHAPE;
   int64_t pairs = 0;
@@ -198,19 +277,41 @@ int rehyat_rope(const rehyat_rope_operand* operands, int n_operands, const rehya
   a.sec2 = axes > 2 ? plan->section[0] + plan->section[1] : rot;
   a.scale = plan->scale;
   a.sign = inverse ? -1.f : 1.f;
-  a.copies_from = rot / 2;
-  a.slots = rot / 2 + (d - rot);
+  // Elements a thread moves at a time: 16 bytes where the rotated and the copied part are made of such pieces, otherwise
+  // two or one.
+  const bool half = plan->layout == REHYAT_ROPE_HALF, in_place = [&] {
+    for (int i = 0; i < n_operands; ++i) {
+      const RopeOperand& o = a.op[i];
+      if (o.x != o.out || o.xb != o.ob || o.xh != o.oh || o.xn != o.on) return false;
+    }
+    return true;
+  }();
+  const int part = half ? rot / 2 : rot, rest = d - rot;
+  int v = (int)(16 / es);
+  if (part % v || rest % v) v = part % 2 || rest % 2 ? 1 : 2;
+  a.d = d;
+  a.copies_from = part / v;
+  a.slots = a.copies_from + (in_place ? 0 : half ? (rest / v + 1) / 2 : rest / v);
   a.N = N;
   a.items = (uint32_t)B * N * a.slots;
-  a.group = 8;
+  // Heads a thread walks over: many, since they share their angles, unless that leaves too few waves.
+  const int64_t waves = (a.items + 63) / 64;
+  auto groups_of = [&](int group) {
+    int n = 0;
+    for (int i = 0; i < n_operands; ++i) n += (a.op[i].heads + group - 1) / group;
+    return n;
+  };
+  a.group = kMostHeads;
+  while (a.group > 1 && waves * groups_of(a.group) < kWaves && groups_of(a.group / 2) <= 65535) a.group /= 2;
+  while (groups_of(a.group) > 65535) a.group *= 2;
   a.groups0 = (a.op[0].heads + a.group - 1) / a.group;
-  const int groups = a.groups0 + (n_operands == 2 ? (a.op[1].heads + a.group - 1) / a.group : 0);
+  const int groups = groups_of(a.group);
   const dim3 grid((a.items + 255) / 256, groups);
   hipStream_t st = (hipStream_t)stream;
   switch (type) {
-    case REHYAT_BF16: launch<Bf16>(a, plan->layout, grid, st); break;
-    case REHYAT_FP16: launch<Fp16>(a, plan->layout, grid, st); break;
-    default: launch<Fp32>(a, plan->layout, grid, st);
+    case REHYAT_BF16: launch<Bf16>(a, plan->layout, v, grid, st); break;
+    case REHYAT_FP16: launch<Fp16>(a, plan->layout, v, grid, st); break;
+    default: launch<Fp32>(a, plan->layout, v, grid, st);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "rotary position kernel launch");

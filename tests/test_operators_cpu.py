@@ -39,7 +39,7 @@ def rope_call(n_ops=1, B=2, N=8, type_=0, inverse=0, heads=3, x=A, out=2 * A, xs
 
 @pytest.mark.parametrize("bad", [
     dict(n_ops=0), dict(n_ops=3), dict(B=0), dict(N=0), dict(type_=3), dict(type_=-1), dict(inverse=2),
-    dict(d=1, rot=2), dict(d=514), dict(rot=66), dict(rot=0), dict(rot=31), dict(layout=2), dict(axes=0), dict(axes=4),
+    dict(d=1, rot=2), dict(d=514), dict(d=65, rot=64), dict(rot=66), dict(rot=0), dict(rot=31), dict(layout=2), dict(axes=0), dict(axes=4),
     dict(section=(31, 0, 0)), dict(axes=2, section=(32, 0, 0)), dict(axes=2, section=(33, -1, 0)), dict(scale=math.inf),
     dict(scale=math.nan), dict(turns=A + 4), dict(x=A + 1), dict(out=A + 1), dict(type_=2, x=A + 2), dict(heads=0),
     dict(heads=65536), dict(xs=(-1, 512, 64)), dict(xs=(1536, 512, 1 << 40)), dict(os_=(1536, 512, 32)),
@@ -87,14 +87,14 @@ def test_turns_are_the_frequencies_modulo_a_turn():
 
 
 @pytest.mark.parametrize("bad", [
-    dict(rot=3), dict(rot=0), dict(rot=130), dict(layout="other"), dict(sections=(32, 31)), dict(sections=(64, 0)),
+    dict(rot=3), dict(rot=0), dict(rot=130), dict(d=129, rot=128), dict(layout="other"), dict(sections=(32, 31)), dict(sections=(64, 0)),
     dict(sections=(16, 16, 16, 16)), dict(scaling=dict(kind="no", factor=2.0)), dict(scaling=dict(kind="linear", factor=0.0)),
     dict(scaling=dict(kind="parts", factor=2.0, original=100, low=2, high=2)), dict(freqs=[1.0]),
     dict(freqs=[1.0] * 64, scaling=dict(kind="linear", factor=2.0)),
 ])
 def test_rope_plan_rejects(bad):
     with pytest.raises(ValueError):
-        binding.Rope(128, device="cpu", **bad)
+        binding.Rope(**{"d": 128, "device": "cpu", **bad})
 
 
 def test_video_plan_splits_the_pairs():
