@@ -6,8 +6,10 @@ if the library is missing or cannot be loaded, importing a symbol from it
 raises.
 """
 import ctypes
+import functools
 import math
 import os
+import struct
 
 import torch
 
@@ -146,8 +148,7 @@ def _load():
     lib.rehyat_rope_turns.restype = ci
     lib.rehyat_rope_turns.argtypes = [ctypes.POINTER(ctypes.c_double), ci, ctypes.POINTER(ctypes.c_uint64)]
     lib.rehyat_rope.restype = ci
-    lib.rehyat_rope.argtypes = [ctypes.POINTER(RopeOperand), ci, ctypes.POINTER(RopePlan),
-                                ctypes.POINTER(RopePositions), ci, ci, ci, ci, vp]
+    lib.rehyat_rope.argtypes = [vp, ci, ctypes.POINTER(RopePlan), vp, ci, ci, ci, ci, vp]   # packed structs
     lib.rehyat_distill_loss_workspace_bytes.restype = ctypes.c_size_t
     lib.rehyat_distill_loss_workspace_bytes.argtypes = [ci, ci, ci, ci]
     lib.rehyat_distill_loss.restype = ci
@@ -531,6 +532,7 @@ class Rope:
         self.turns = turns.to(device)
         self._plan = RopePlan(self.turns.data_ptr(), d, rot, ROPE_LAYOUTS[layout], len(sections),
                               (ctypes.c_int32 * 3)(*sections), self.scale)
+        self._ref = ctypes.byref(self._plan)
 
     @staticmethod
     def _frequencies(n, base, scaling):
@@ -562,20 +564,30 @@ class Rope:
                    device=device)
 
 
+# rehyat_rope_operand (two of them) and rehyat_rope_positions as they lie in memory: packed in one go, 13.5 -> XX us a call
+_rope_operands = struct.Struct("QQ6qi4x" * 2)
+_rope_positions = struct.Struct("Q3q3i4x")
+_NO_OPERAND = (0,) * 9
+
+
 def _rope_operand(x, out, plan, like):
     if x.dim() != 4 or x.dtype not in _TYPES or not x.is_cuda or x.stride(3) != 1:
         raise TypeError("q and k must be CUDA tensors [B, H, N, d] in bf16, fp16 or fp32 with contiguous rows")
-    B, H, N, d = x.shape
+    B, H, N, d = shape = x.shape
     if d != plan.d or (like is not None and (like.shape[0], like.shape[2]) != (B, N)):
         raise ValueError("q and k must have the plan's head width, and one number of sequences and tokens")
     if like is not None and (like.dtype != x.dtype or like.device != x.device):
         raise TypeError("q and k must be of one type and on one device")
+    xb, xh, xn, _ = x.stride()
     if out is None:
-        out = torch.empty((B, H, N, d), device=x.device, dtype=x.dtype)
-    elif out.shape != x.shape or out.dtype != x.dtype or out.device != x.device or out.stride(3) != 1:
-        raise TypeError("out must match its operand, with contiguous rows")
-    (xb, xh, xn, _), (ob, oh, on, _) = x.stride(), out.stride()
-    return RopeOperand(x.data_ptr(), out.data_ptr(), xb, xh, xn, ob, oh, on, H), out
+        out = torch.empty(shape, device=x.device, dtype=x.dtype)
+        n = N * d
+        ob, oh, on = n * H, n, d
+    else:
+        if out.shape != shape or out.dtype != x.dtype or out.device != x.device or out.stride(3) != 1:
+            raise TypeError("out must match its operand, with contiguous rows")
+        ob, oh, on, _ = out.stride()
+    return (x.data_ptr(), out.data_ptr(), xb, xh, xn, ob, oh, on, H), out
 
 
 def rope(q, k, plan, grid=None, start=0, positions=None, inverse=False, out=None, stream=None):
@@ -592,18 +604,14 @@ def rope(q, k, plan, grid=None, start=0, positions=None, inverse=False, out=None
     if ctx is not None:
         with ctx:
             return rope(q, k, plan, grid, start, positions, inverse, out)
-    lib = _load()
-    outs = (None, None) if out is None else (out if isinstance(out, (tuple, list)) else (out, None))
-    ops = (RopeOperand * 2)()
-    ops[0], q_out = _rope_operand(q, outs[0], plan, None)
-    k_out = None
-    if k is not None:
-        ops[1], k_out = _rope_operand(k, outs[1], plan, q)
+    q_out, k_out = (None, None) if out is None else (out if isinstance(out, (tuple, list)) else (out, None))
+    q_op, q_out = _rope_operand(q, q_out, plan, None)
+    k_op, k_out = (_NO_OPERAND, None) if k is None else _rope_operand(k, k_out, plan, q)
     if plan.turns.device != q.device:
         raise ValueError("the plan is on another device than the tensors")
     B, _, N, _ = q.shape
     axes = len(plan.sections)
-    pos = RopePositions(start=int(start))
+    at = bits = rows = cols = stride_b = stride_n = 0
     if positions is not None:
         if grid is not None or start != 0:
             raise ValueError("give either positions or a grid and a start")
@@ -613,23 +621,25 @@ def rope(q, k, plan, grid=None, start=0, positions=None, inverse=False, out=None
         if tuple(positions.shape) not in ((N,) + tail, (B, N) + tail) or (tail and positions.stride(-1) != 1):
             raise ValueError(f"positions must have shape {(N,) + tail} or {(B, N) + tail}")
         strides = positions.stride()[:positions.dim() - len(tail)]
-        pos.data, pos.bits = positions.data_ptr(), 32 if positions.dtype == torch.int32 else 64
-        pos.stride_b, pos.stride_n = strides if len(strides) == 2 else (0, strides[0])
+        at, bits = positions.data_ptr(), 32 if positions.dtype == torch.int32 else 64
+        stride_b, stride_n = strides if len(strides) == 2 else (0, strides[0])
     elif axes > 1:
         if grid is None or len(grid) != axes - 1:
             raise ValueError(f"a plan of {axes} axes needs a grid of {axes - 1} sizes, or positions")
-        if not all(1 <= int(n) < 2**31 for n in grid):
+        rows, cols = (0, int(grid[0])) if axes == 2 else (int(grid[0]), int(grid[1]))
+        if not (1 <= cols < 2**31 and (axes == 2 or 1 <= rows < 2**31)):
             raise ValueError("the sizes of a grid must be positive and fit 32 bits")
-        pos.rows, pos.cols = (0, int(grid[0])) if axes == 2 else (int(grid[0]), int(grid[1]))
     elif grid is not None:
         raise ValueError("a plan of one axis takes no grid")
-    rc = lib.rehyat_rope(ops, 1 if k is None else 2, ctypes.byref(plan._plan), ctypes.byref(pos), B, N,
-                         _TYPES[q.dtype], int(bool(inverse)), _stream_handle(None))
+    rc = _load().rehyat_rope(_rope_operands.pack(*q_op, *k_op), 1 if k is None else 2, plan._ref,
+                             _rope_positions.pack(at, stride_b, stride_n, int(start), bits, rows, cols), B, N,
+                             _TYPES[q.dtype], 1 if inverse else 0, _stream_handle(None))
     if rc != OK:
         raise RehyatError(rc, "rehyat_rope")
     return q_out if k is None else (q_out, k_out)
 
 
+@functools.lru_cache(maxsize=1024)
 def distill_loss_workspace_bytes(B, H, N, d):
     return _load().rehyat_distill_loss_workspace_bytes(B, H, N, d)
 
@@ -665,15 +675,14 @@ def distill_loss(y_hat, y, scale=None, weight=None, grad=None, loss=None, worksp
     elif loss.numel() != 1 or loss.dtype != torch.float32 or loss.device != dev:
         raise TypeError("loss must be one CUDA fp32")
     if workspace is None:
-        workspace = torch.empty(lib.rehyat_distill_loss_workspace_bytes(B, H, N, d), device=dev, dtype=torch.uint8)
+        workspace = torch.empty(distill_loss_workspace_bytes(B, H, N, d), device=dev, dtype=torch.uint8)
     elif workspace.device != dev or not workspace.is_contiguous():
         raise TypeError("workspace must be a contiguous tensor on y_hat's device")
     if scale is None:
         scale = 1.0 / max(1, y_hat.numel())
     rc = lib.rehyat_distill_loss(y_hat.data_ptr(), y.data_ptr(), _TYPES[y.dtype],
                                  None if weight is None else weight.data_ptr(), scale, grad.data_ptr(), loss.data_ptr(),
-                                 B, H, N, d, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                 _stream_handle(None))
+                                 B, H, N, d, workspace.data_ptr(), workspace.nbytes, _stream_handle(None))
     if rc != OK:
         raise RehyatError(rc, "rehyat_distill_loss")
     return loss, grad

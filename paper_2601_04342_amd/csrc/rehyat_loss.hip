@@ -12,6 +12,7 @@ namespace rehyat {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kSmall = 32768, kSmallRows = 4;   // elements and rows up to which one workgroup does it all
 
 struct LossArgs {
   const uint16_t* y_hat;
@@ -19,6 +20,7 @@ struct LossArgs {
   const float* weight;   // [B, N] or null
   uint16_t* grad;
   double* partial;       // [rows, pieces]
+  float* loss;
   float scale;
   int64_t row;           // elements of a row of pieces: N d of one (b, h), or everything where there are no weights
   int64_t piece;         // elements of a piece
@@ -53,22 +55,86 @@ __device__ __forceinline__ float element(float y_hat, float y, float w, uint16_t
   return __builtin_fabsf(diff) * w;
 }
 
+// Eight elements of a row: their part of the sum, and their gradients.  Rows of (b, h)s of an odd size begin anywhere.
+constexpr int kVec = 8;
+template <typename E>
+struct Eight {
+  typedef uint16_t u16x8 __attribute__((ext_vector_type(8), aligned(2)));
+  typedef typename E::store teacher __attribute__((ext_vector_type(8), aligned(sizeof(typename E::store))));
+  u16x8 y_hat;
+  teacher y;
+  float w;
+  __device__ __forceinline__ float run(float scale, uint16_t* grad) const {
+    const float up = w * scale;
+    const uint16_t gu = Bf16::put(up), gd = Bf16::put(-up);
+    u16x8 g;
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) {
+      uint16_t one;
+      sum += element(Bf16::get(y_hat[k]), E::get(y[k]), w, gu, gd, &one);
+      g[k] = one;
+    }
+    *(u16x8*)grad = g;
+    return sum;
+  }
+};
+
+// A workgroup takes elements [lo, hi) of row `r`; its sum on thread 0.
+template <typename E, int THREADS>
+__device__ __forceinline__ double loss_piece(const LossArgs& a, int64_t r, int64_t lo, int64_t hi) {
+  typedef typename E::store T;
+  typedef Eight<E> V;
+  const uint16_t* const y_hat = a.y_hat + r * a.row;
+  const T* const y = (const T*)a.y + r * a.row;
+  uint16_t* const grad = a.grad + r * a.row;
+  const float* const weight = a.weight ? a.weight + (int64_t)((uint32_t)r / (uint32_t)a.H) * a.N : nullptr;
+  auto weight_of = [&](int64_t i) { return weight ? weight[(uint32_t)i / (uint32_t)a.d] : 1.f; };
+  double sum = 0;
+  int64_t i = lo;
+  if (!weight || a.d % kVec == 0) {   // eight elements have one weight (lo is a multiple of 8)
+    constexpr int kStep = THREADS * kVec;
+    auto fetch = [&](int64_t at) {
+      V x;
+      x.y_hat = *(const typename V::u16x8*)(y_hat + at);
+      x.y = *(const typename V::teacher*)(y + at);
+      x.w = weight_of(at);
+      return x;
+    };
+    int64_t at = lo + threadIdx.x * kVec;
+    for (; at + kStep + kVec <= hi; at += 2 * kStep) {   // two in flight
+      const V x = fetch(at), z = fetch(at + kStep);
+      sum += x.run(a.scale, grad + at);
+      sum += z.run(a.scale, grad + at + kStep);
+    }
+    if (at + kVec <= hi) sum += fetch(at).run(a.scale, grad + at);
+    i = lo + (hi - lo) / kVec * kVec;
+  }
+  for (i += threadIdx.x; i < hi; i += THREADS) {
+    const float w = weight_of(i), up = w * a.scale;
+    uint16_t g;
+    sum += element(Bf16::get(y_hat[i]), E::get(y[i]), w, Bf16::put(up), Bf16::put(-up), &g);
+    grad[i] = g;
+  }
+  return block_sum<THREADS>(sum);
+}
+
 template <typename E>
 __global__ __launch_bounds__(kThreads) void loss_kernel(LossArgs a) {
-  typedef typename E::store T;
   const int64_t lo = blockIdx.x * a.piece, hi = lo + a.piece < a.row ? lo + a.piece : a.row;
-  const int64_t base = blockIdx.y * a.row;
-  const float* weight = a.weight ? a.weight + (int64_t)(blockIdx.y / a.H) * a.N : nullptr;
-  double sum = 0;
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) {
-    const float w = weight ? weight[(uint32_t)i / (uint32_t)a.d] : 1.f;
-    const float up = weight ? w * a.scale : a.scale;
-    uint16_t g;
-    sum += element(Bf16::get(a.y_hat[base + i]), E::get(((const T*)a.y)[base + i]), w, Bf16::put(up), Bf16::put(-up), &g);
-    a.grad[base + i] = g;
-  }
-  sum = block_sum<kThreads>(sum);
+  const double sum = loss_piece<E, kThreads>(a, blockIdx.y, lo, hi);
   if (threadIdx.x == 0) a.partial[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sum;
+}
+
+// Few elements: one workgroup, one launch.
+template <typename E>
+__global__ __launch_bounds__(1024) void loss_small_kernel(LossArgs a, int rows) {
+  double sum = 0;
+  for (int r = 0; r < rows; ++r) {
+    sum += loss_piece<E, 1024>(a, r, 0, a.row);
+    __syncthreads();   // the sums' shared memory
+  }
+  if (threadIdx.x == 0) *a.loss = (float)(sum * a.scale);
 }
 
 __global__ __launch_bounds__(1024) void loss_finish_kernel(const double* partial, int n, float scale, float* loss) {
@@ -128,16 +194,28 @@ int rehyat_distill_loss(const void* y_hat, const void* y, int type, const float*
   a.d = d;
   const int64_t rows = weight ? (int64_t)B * H : 1;
   a.row = weight ? (int64_t)N * d : (int64_t)B * H * N * d;
+  a.loss = loss;
+  hipStream_t st = (hipStream_t)stream;
+  hipError_t e;
+  if (rows * a.row <= kSmall && rows <= kSmallRows) {
+    switch (type) {
+      case REHYAT_BF16: loss_small_kernel<Bf16><<<1, 1024, 0, st>>>(a, (int)rows); break;
+      case REHYAT_FP16: loss_small_kernel<Fp16><<<1, 1024, 0, st>>>(a, (int)rows); break;
+      default: loss_small_kernel<Fp32><<<1, 1024, 0, st>>>(a, (int)rows);
+    }
+    e = hipGetLastError();
+    if (e != hipSuccess) return hip_fail(e, "loss kernel launch");
+    return REHYAT_OK;
+  }
   int64_t pieces;
   cut(rows, a.row, &a.piece, &pieces);
   const dim3 grid((unsigned)pieces, (unsigned)rows);
-  hipStream_t st = (hipStream_t)stream;
   switch (type) {
     case REHYAT_BF16: loss_kernel<Bf16><<<grid, kThreads, 0, st>>>(a); break;
     case REHYAT_FP16: loss_kernel<Fp16><<<grid, kThreads, 0, st>>>(a); break;
     default: loss_kernel<Fp32><<<grid, kThreads, 0, st>>>(a);
   }
-  hipError_t e = hipGetLastError();
+  e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "loss kernel launch");
   loss_finish_kernel<<<1, 1024, 0, st>>>(a.partial, (int)(pieces * rows), scale, loss);
   e = hipGetLastError();

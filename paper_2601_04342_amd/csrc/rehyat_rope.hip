@@ -15,7 +15,7 @@
 namespace rehyat {
 namespace {
 
-constexpr int kMostHeads = 16, kWaves = 4096;
+constexpr int kMostHeads = 16, kWaves = 8192;
 
 struct RopeOperand {
   const void* x;
