@@ -564,7 +564,7 @@ class Rope:
                    device=device)
 
 
-# rehyat_rope_operand (two of them) and rehyat_rope_positions as they lie in memory: packed in one go, 13.5 -> XX us a call
+# rehyat_rope_operand (two of them) and rehyat_rope_positions as they lie in memory: packed in one go (as ctypes structs 1.2 us a call more)
 _rope_operands = struct.Struct("QQ6qi4x" * 2)
 _rope_positions = struct.Struct("Q3q3i4x")
 _NO_OPERAND = (0,) * 9
@@ -580,7 +580,7 @@ def _rope_operand(x, out, plan, like):
         raise TypeError("q and k must be of one type and on one device")
     xb, xh, xn, _ = x.stride()
     if out is None:
-        out = torch.empty(shape, device=x.device, dtype=x.dtype)
+        out = x.new_empty(shape)
         n = N * d
         ob, oh, on = n * H, n, d
     else:

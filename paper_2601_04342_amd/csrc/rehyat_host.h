@@ -16,6 +16,10 @@ inline bool aligned16(const void* p) { return aligned(p, 16); }
 inline bool aligned4(const void* p) { return aligned(p, 4); }
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// Whether a pass over so many bytes goes past the caches (non-temporal loads and stores): what does not fit the 256 MB in
+// front of the memory is gone when the next pass comes, and what fits is there.  Each user has both sides measured.
+inline bool past_caches(int64_t bytes) { return bytes > ((int64_t)256 << 20); }
+
 inline bool valid_type(int t) { return t == REHYAT_BF16 || t == REHYAT_FP16 || t == REHYAT_FP32; }
 inline size_t type_bytes(int t) { return t == REHYAT_FP32 ? 4 : 2; }
 
