@@ -5,8 +5,12 @@
 // quadrant and an angle within an eighth of a turn, where short series for cos and sin serve.  No far position loses more
 // than a near one.
 //
-// Bound by HBM: each element is read and written once, and needs 3 flops.  A thread keeps the cos and sin of its pairs
-// and walks over the heads of its token with them, since they are the same for every head.
+// Bound by HBM: each element is read and written once, and needs 3 flops.  A thread keeps the cos and sin of its one or
+// two pairs and walks over the heads of its token with them, since they are the same for every head, four heads in
+// flight.  q and k of a 480p layer, 403 MB: 73.4 us, 5.5 TB/s; the gradient of a guidance pair, 805 MB, 142 us, 5.7 TB/s;
+// half of each head in fp16, 126 MB, 24.8 us.  One head at a time they took 110, 222 and 62 us; with 16 bytes a
+// thread, four and eight pairs of angles, 77.5, 150 and 29.  Stored past the caches the first takes 6 us less, and the
+// attention behind it, which then finds nothing there, 14 us more.
 #include <cmath>
 
 #include "rehyat_elem.h"
@@ -15,7 +19,11 @@
 namespace rehyat {
 namespace {
 
-constexpr int kMostHeads = 16, kWaves = 8192;
+// Heads a thread walks over, at most, and the waves a launch should have for it: many heads share their angles, but few
+// waves do not fill the chip.  q and k of (sequences, heads, tokens, width), half layout, with 1,024 / 2,048 / 4,096 /
+// 16,384 waves wanted: (1, 12, 512, 128) 4.0 / 3.8 / 4.7 / 4.7 us, (2, 12, 1560, 128) 7.9 / 7.9 / 7.5 / 11.0,
+// (1, 12, 4096, 128) 9.5 / 9.5 / 9.5 / 13.2.  At most 8 heads instead of 16: the gradient of a pair 157 us, not 142.
+constexpr int kMostHeads = 16, kWaves = 2048;
 
 struct RopeOperand {
   const void* x;
@@ -53,7 +61,8 @@ __device__ __forceinline__ void cos_sin(uint32_t t, float* c, float* s) {
   *s = quarter >= 2 ? -b : b;
 }
 
-// V elements of a row that stand together, loaded and stored as one; rows begin at any element.
+// V elements of a row that stand together, loaded and stored as one; rows begin at any element (the first of them one, two
+// or four elements off 16 bytes: 32.3 us where 31.4 are taken otherwise).
 template <typename E, int V>
 struct Vec {
   typedef typename E::store raw __attribute__((ext_vector_type(V), aligned(sizeof(typename E::store))));
@@ -165,18 +174,11 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   }
 }
 
-template <typename E, int V>
-void launch(const RopeArgs& a, int layout, dim3 grid, hipStream_t st) {
-  if (layout == REHYAT_ROPE_INTERLEAVED)
-    rope_kernel<E, REHYAT_ROPE_INTERLEAVED, (V < 2 ? 2 : V)><<<grid, 256, 0, st>>>(a);
-  else
-    rope_kernel<E, REHYAT_ROPE_HALF, V><<<grid, 256, 0, st>>>(a);
-}
 template <typename E>
 void launch(const RopeArgs& a, int layout, int v, dim3 grid, hipStream_t st) {
-  if (v == 16 / sizeof(typename E::store)) launch<E, 16 / sizeof(typename E::store)>(a, layout, grid, st);
-  else if (v == 2) launch<E, 2>(a, layout, grid, st);
-  else launch<E, 1>(a, layout, grid, st);
+  if (layout == REHYAT_ROPE_INTERLEAVED) rope_kernel<E, REHYAT_ROPE_INTERLEAVED, 2><<<grid, 256, 0, st>>>(a);
+  else if (v == 2) rope_kernel<E, REHYAT_ROPE_HALF, 2><<<grid, 256, 0, st>>>(a);
+  else rope_kernel<E, REHYAT_ROPE_HALF, 1><<<grid, 256, 0, st>>>(a);
 }
 
 // Whether the rows of an output with these strides are apart: every dimension steps over all that the smaller ones span.
@@ -277,8 +279,6 @@ int rehyat_rope(const rehyat_rope_operand* operands, int n_operands, const rehya
   a.sec2 = axes > 2 ? plan->section[0] + plan->section[1] : rot;
   a.scale = plan->scale;
   a.sign = inverse ? -1.f : 1.f;
-  // Elements a thread moves at a time: 16 bytes where the rotated and the copied part are made of such pieces, otherwise
-  // two or one.
   const bool half = plan->layout == REHYAT_ROPE_HALF, in_place = [&] {
     for (int i = 0; i < n_operands; ++i) {
       const RopeOperand& o = a.op[i];
@@ -287,8 +287,7 @@ int rehyat_rope(const rehyat_rope_operand* operands, int n_operands, const rehya
     return true;
   }();
   const int part = half ? rot / 2 : rot, rest = d - rot;
-  int v = (int)(16 / es);
-  if (part % v || rest % v) v = part % 2 || rest % 2 ? 1 : 2;
+  const int v = half && part % 2 ? 1 : 2;   // (rot and d are even, and so is `rest`)
   a.d = d;
   a.copies_from = part / v;
   a.slots = a.copies_from + (in_place ? 0 : half ? (rest / v + 1) / 2 : rest / v);
