@@ -353,8 +353,10 @@ int rehyat_step(const void *q_t, const void *k_win, const void *v_win,
  *   each of B x N tokens.  Strides in elements (>= 0; those of x may be 0), rows
  *   themselves contiguous, pointers aligned to an element: token-major projections
  *   can be read and head-major attention operands, or rows of a K window, written.
- *   out is x itself (same strides) or does not overlap it; rows of out do not
- *   overlap each other.
+ *   out is x itself (same strides) or does not overlap it, the other operand's x or
+ *   its out (they may lie between each other's rows where their strides are the same:
+ *   queries and keys of one projection, in place); rows of out do not overlap each
+ *   other.
  *
  * One or two operands (queries; keys, whose number of heads may differ) of one
  * `type` (REHYAT_BF16 / FP16 / FP32) are turned in one launch.  N may be 1 (one

@@ -610,6 +610,8 @@ def rope(q, k, plan, grid=None, start=0, positions=None, inverse=False, out=None
     if plan.turns.device != q.device:
         raise ValueError("the plan is on another device than the tensors")
     B, _, N, _ = q.shape
+    if not -2**63 <= start < 2**63:
+        raise ValueError("start must fit 64 bits")
     axes = len(plan.sections)
     at = bits = rows = cols = stride_b = stride_n = 0
     if positions is not None:

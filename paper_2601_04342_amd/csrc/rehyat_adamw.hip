@@ -525,6 +525,11 @@ int rehyat_adamw_moments(const void* m, const void* m_exp, const void* v, const 
   if (!m || !m_exp || !v || !v_exp || !m_out || !v_out) return REHYAT_E_NULL;
   if (n < 1 || n >= ((int64_t)1 << 38)) return REHYAT_E_SHAPE;
   if (!aligned16(m) || !aligned16(v) || !aligned16(m_out) || !aligned16(v_out)) return REHYAT_E_SHAPE;
+  const int64_t groups = (n + kGroup - 1) / kGroup;
+  Range ranges[] = {{(uintptr_t)m, (uintptr_t)m + kGroup * groups, false}, {(uintptr_t)v, (uintptr_t)v + kGroup * groups, false},
+                    {(uintptr_t)m_exp, (uintptr_t)m_exp + groups, false}, {(uintptr_t)v_exp, (uintptr_t)v_exp + groups, false},
+                    {(uintptr_t)m_out, (uintptr_t)m_out + 4 * n, true}, {(uintptr_t)v_out, (uintptr_t)v_out + 4 * n, true}};
+  if (!apart(ranges, 6)) return REHYAT_E_SHAPE;
   auto* const kernel = past_caches(10 * n) ? adamw_moments_kernel<true> : adamw_moments_kernel<false>;
   kernel<<<(unsigned)((n + 4 * kThreads - 1) / (4 * kThreads)), kThreads, 0, (hipStream_t)stream>>>(
       (const uint8_t*)m, (const uint8_t*)m_exp, (const uint8_t*)v, (const uint8_t*)v_exp, m_out, v_out, n);

@@ -16,6 +16,11 @@ inline bool aligned16(const void* p) { return aligned(p, 16); }
 inline bool aligned4(const void* p) { return aligned(p, 4); }
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// Whether two ranges of bytes are apart.
+inline bool ranges_apart(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  return (uintptr_t)a + (uintptr_t)a_bytes <= (uintptr_t)b || (uintptr_t)b + (uintptr_t)b_bytes <= (uintptr_t)a;
+}
+
 // Whether a pass over so many bytes goes past the caches (non-temporal loads and stores): what does not fit the 256 MB in
 // front of the memory is gone when the next pass comes, and what fits is there.  Each user has both sides measured.
 inline bool past_caches(int64_t bytes) { return bytes > ((int64_t)256 << 20); }

@@ -185,6 +185,10 @@ int rehyat_distill_loss(const void* y_hat, const void* y, int type, const float*
   if (!sizes_ok(B, H, N, d) || !valid_type(type) || !std::isfinite(scale)) return REHYAT_E_SHAPE;
   if (!aligned16(y_hat) || !aligned16(y) || !aligned16(grad) || !aligned4(loss) || (weight && !aligned4(weight)))
     return REHYAT_E_SHAPE;
+  const int64_t n = (int64_t)B * H * N * d;
+  if (!ranges_apart(grad, 2 * n, y_hat, 2 * n) || !ranges_apart(grad, 2 * n, y, n * (int64_t)type_bytes(type)) ||
+      (weight && !ranges_apart(grad, 2 * n, weight, (int64_t)4 * B * N)))
+    return REHYAT_E_SHAPE;
   if (!aligned(workspace, 256) || workspace_bytes < rehyat_distill_loss_workspace_bytes(B, H, N, d))
     return REHYAT_E_WORKSPACE;
   LossArgs a;
@@ -198,7 +202,7 @@ int rehyat_distill_loss(const void* y_hat, const void* y, int type, const float*
   a.N = N;
   a.d = d;
   const int64_t rows = weight ? (int64_t)B * H : 1;
-  a.row = weight ? (int64_t)N * d : (int64_t)B * H * N * d;
+  a.row = weight ? (int64_t)N * d : n;
   a.loss = loss;
   hipStream_t st = (hipStream_t)stream;
   hipError_t e;

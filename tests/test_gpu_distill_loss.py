@@ -190,3 +190,14 @@ def test_refusals():
         binding.distill_loss(y_hat, y, workspace=torch.empty(8, device="cuda", dtype=torch.uint8))
     assert e.value.code == binding.E_WORKSPACE
     torch.cuda.synchronize()
+
+
+def test_nothing_and_overlaps_are_refused():
+    y_hat, y = (t.cuda() for t in inputs(1, 2, 8, 64, BF16, 12))
+    with pytest.raises(binding.RehyatError):
+        binding.distill_loss(y_hat[:, :, :0].contiguous(), y[:, :, :0].contiguous())
+    for grad in (y_hat, y):                       # the gradient over what is read
+        with pytest.raises(binding.RehyatError) as e:
+            binding.distill_loss(y_hat, y, grad=grad)
+        assert e.value.code == binding.E_SHAPE
+    torch.cuda.synchronize()

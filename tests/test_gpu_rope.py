@@ -342,3 +342,37 @@ def test_refusals_on_the_device_side_of_the_binding():
         binding.rope(q, None, plan, out=torch.empty(2, 1, 8, 64, device="cuda", dtype=BF16).expand(2, 3, 8, 64))
     assert e.value.code == binding.E_SHAPE
     torch.cuda.synchronize()
+
+
+def test_queries_and_keys_of_one_projection_in_place():
+    """Each in place, between the other's rows; the values beside them stay."""
+    B, H, N, d = 2, 3, 40, 64
+    plan = binding.Rope(d)
+    qkv = operand(B, 3 * H, N, d, BF16, 17).transpose(1, 2).reshape(B, N, 3, H, d).contiguous()
+    was = qkv.clone()
+    q, k, v = (qkv[:, :, i].transpose(1, 2) for i in range(3))
+    want = binding.rope(q, k, plan, start=7)
+    binding.rope(q, k, plan, start=7, out=(q, k))
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(qkv[:, :, 2], was[:, :, 2])
+    for out in ((k, q), (q, q), (v, q)):     # exchanged, one for both, onto what the other reads
+        with pytest.raises(binding.RehyatError) as e:
+            binding.rope(q, k, plan, out=out)
+        assert e.value.code == binding.E_SHAPE
+    torch.cuda.synchronize()
+
+
+def test_queries_and_keys_that_are_one_tensor():
+    plan = binding.Rope(64)
+    x = operand(1, 2, 30, 64, BF16, 18)
+    a, b = binding.rope(x, x, plan, start=2)
+    assert torch.equal(a, b) and torch.equal(a, binding.rope(x, None, plan, start=2))
+
+
+def test_nothing_to_rotate_is_refused():
+    plan = binding.Rope(64)
+    x = operand(2, 3, 8, 64, BF16, 19)
+    for empty in (x[:0], x[:, :0], x[:, :, :0]):
+        with pytest.raises(binding.RehyatError):
+            binding.rope(empty, None, plan)
+    with pytest.raises(ValueError):
+        binding.rope(x, None, plan, start=2**63)
