@@ -564,30 +564,24 @@ class Rope:
                    device=device)
 
 
-# rehyat_rope_operand (two of them) and rehyat_rope_positions as they lie in memory: packed in one go (as ctypes structs 1.2 us a call more)
+# rehyat_rope_operand (two of them) and rehyat_rope_positions as they lie in memory, packed in one go: a call for one token
+# is 12 us of host work, 3 of them the launch, and was 13.5 with a ctypes struct for each
 _rope_operands = struct.Struct("QQ6qi4x" * 2)
 _rope_positions = struct.Struct("Q3q3i4x")
 _NO_OPERAND = (0,) * 9
+_ROPE_OPERAND = "q and k must be CUDA tensors [B, H, N, d] in bf16, fp16 or fp32 with contiguous rows"
 
 
-def _rope_operand(x, out, plan, like):
-    if x.dim() != 4 or x.dtype not in _TYPES or not x.is_cuda or x.stride(3) != 1:
-        raise TypeError("q and k must be CUDA tensors [B, H, N, d] in bf16, fp16 or fp32 with contiguous rows")
-    B, H, N, d = shape = x.shape
-    if d != plan.d or (like is not None and (like.shape[0], like.shape[2]) != (B, N)):
-        raise ValueError("q and k must have the plan's head width, and one number of sequences and tokens")
-    if like is not None and (like.dtype != x.dtype or like.device != x.device):
-        raise TypeError("q and k must be of one type and on one device")
-    xb, xh, xn, _ = x.stride()
+def _rope_operand(x, shape, stride, out):
+    """The fields of a rehyat_rope_operand, and its output."""
+    _, H, N, d = shape
     if out is None:
-        out = x.new_empty(shape)
-        n = N * d
-        ob, oh, on = n * H, n, d
-    else:
-        if out.shape != shape or out.dtype != x.dtype or out.device != x.device or out.stride(3) != 1:
-            raise TypeError("out must match its operand, with contiguous rows")
-        ob, oh, on, _ = out.stride()
-    return (x.data_ptr(), out.data_ptr(), xb, xh, xn, ob, oh, on, H), out
+        out, n = x.new_empty(shape), N * d
+        return (x.data_ptr(), out.data_ptr(), *stride[:3], n * H, n, d, H), out
+    to = out.stride()
+    if out.shape != shape or out.dtype != x.dtype or out.device != x.device or to[3] != 1:
+        raise TypeError("out must match its operand, with contiguous rows")
+    return (x.data_ptr(), out.data_ptr(), *stride[:3], *to[:3], H), out
 
 
 def rope(q, k, plan, grid=None, start=0, positions=None, inverse=False, out=None, stream=None):
@@ -600,16 +594,32 @@ def rope(q, k, plan, grid=None, start=0, positions=None, inverse=False, out=None
     n // cols % rows, column n % cols; with two axes and grid=(cols,) at (start + n // cols, n % cols); with one at
     start + n.  ``inverse=True`` turns back, which is also the gradient.  ``out``: tensors to write, of any strides (a
     part of a K window), or the operands themselves; new contiguous ones by default.  Returns (q', k'), or q' without k."""
-    ctx = _elsewhere(q, stream) if q.is_cuda else None
+    kind = _TYPES.get(q.dtype)
+    if kind is None or not q.is_cuda or q.dim() != 4:
+        raise TypeError(_ROPE_OPERAND)
+    ctx = _elsewhere(q, stream)
     if ctx is not None:
         with ctx:
             return rope(q, k, plan, grid, start, positions, inverse, out)
-    q_out, k_out = (None, None) if out is None else (out if isinstance(out, (tuple, list)) else (out, None))
-    q_op, q_out = _rope_operand(q, q_out, plan, None)
-    k_op, k_out = (_NO_OPERAND, None) if k is None else _rope_operand(k, k_out, plan, q)
+    shape, stride = q.shape, q.stride()
+    B, _, N, d = shape
+    if stride[3] != 1:
+        raise TypeError(_ROPE_OPERAND)
+    if d != plan.d:
+        raise ValueError("q and k must have the plan's head width")
     if plan.turns.device != q.device:
         raise ValueError("the plan is on another device than the tensors")
-    B, _, N, _ = q.shape
+    q_out, k_out = (None, None) if out is None else (out if isinstance(out, (tuple, list)) else (out, None))
+    q_op, q_out = _rope_operand(q, shape, stride, q_out)
+    if k is None:
+        k_op = _NO_OPERAND
+    else:
+        k_shape, k_stride = k.shape, k.stride()
+        if k.dtype != q.dtype or k.device != q.device or len(k_shape) != 4 or k_stride[3] != 1:
+            raise TypeError(_ROPE_OPERAND + ", of one type and on one device")
+        if k_shape[0] != B or k_shape[2] != N or k_shape[3] != d:
+            raise ValueError("q and k must have one head width, number of sequences and number of tokens")
+        k_op, k_out = _rope_operand(k, k_shape, k_stride, k_out)
     if not -2**63 <= start < 2**63:
         raise ValueError("start must fit 64 bits")
     axes = len(plan.sections)
@@ -620,11 +630,11 @@ def rope(q, k, plan, grid=None, start=0, positions=None, inverse=False, out=None
         tail = () if axes == 1 else (axes,)
         if positions.dtype not in (torch.int32, torch.int64) or positions.device != q.device:
             raise TypeError("positions must be int32 or int64 on the tensors' device")
-        if tuple(positions.shape) not in ((N,) + tail, (B, N) + tail) or (tail and positions.stride(-1) != 1):
+        strides = positions.stride()
+        if positions.shape not in ((N,) + tail, (B, N) + tail) or (tail and strides[-1] != 1):
             raise ValueError(f"positions must have shape {(N,) + tail} or {(B, N) + tail}")
-        strides = positions.stride()[:positions.dim() - len(tail)]
         at, bits = positions.data_ptr(), 32 if positions.dtype == torch.int32 else 64
-        stride_b, stride_n = strides if len(strides) == 2 else (0, strides[0])
+        stride_b, stride_n = strides[:2] if len(strides) == 2 + len(tail) else (0, strides[0])
     elif axes > 1:
         if grid is None or len(grid) != axes - 1:
             raise ValueError(f"a plan of {axes} axes needs a grid of {axes - 1} sizes, or positions")
@@ -635,7 +645,7 @@ def rope(q, k, plan, grid=None, start=0, positions=None, inverse=False, out=None
         raise ValueError("a plan of one axis takes no grid")
     rc = _load().rehyat_rope(_rope_operands.pack(*q_op, *k_op), 1 if k is None else 2, plan._ref,
                              _rope_positions.pack(at, stride_b, stride_n, int(start), bits, rows, cols), B, N,
-                             _TYPES[q.dtype], 1 if inverse else 0, _stream_handle(None))
+                             kind, 1 if inverse else 0, _stream_handle(None))
     if rc != OK:
         raise RehyatError(rc, "rehyat_rope")
     return q_out if k is None else (q_out, k_out)

@@ -345,7 +345,7 @@ def test_adamw_binding_rejects_host_tensors():
 
 
 def test_host_layers_under_asan_ubsan(tmp_path):
-    """The drivers' calls are all rejected, or answered, before the first HIP call; device code is compiled as usual."""
+    """Every call of the program is rejected, or answered, before the first HIP call; device code is compiled as usual."""
     if not os.path.exists(build.HIPCC):
         pytest.skip("hipcc not available")
     exe = str(tmp_path / "operators_san")
