@@ -444,7 +444,7 @@ int rehyat_distill_loss(const void *y_hat, const void *y, int type,
  *                       of v is an fp32 number without sign whose leading 11 bits
  *                       are c + 8 (v_exp - 30); 0 is 0.  Exponent 255: no element
  *                       of the group is a number any more (a gradient was not
- *                       finite, or a moment passed 2^127).
+ *                       finite, or a moment passed 2^127); bytes of v are 255 then.
  *                       The new moments are rounded once to fp32 (so from 1 - beta1
  *                       and 1 - beta2 in fp32), enter the update, and are rounded
  *                       from there to 8 bits, to nearest; a v that is not 0 never

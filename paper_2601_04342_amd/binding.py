@@ -539,8 +539,8 @@ class Rope:
         """n frequencies of one axis in 64 bits, and the factor on rotated values."""
         if scaling is None:
             return base ** (-torch.arange(n, dtype=torch.float64) / n), 1.0
-        kind, s = scaling["kind"], float(scaling["factor"])
-        if kind not in ("linear", "base", "parts") or not s > 0:
+        kind, s = scaling.get("kind"), float(scaling.get("factor", 0.0))
+        if kind not in ("linear", "base", "parts") or not 0 < s < math.inf:
             raise ValueError('scaling needs kind "linear", "base" or "parts" and a positive factor')
         if kind == "base" and n > 1:
             base *= s ** (n / (n - 1))
@@ -550,9 +550,10 @@ class Rope:
         if kind == "base":
             return f, 1.0
         low, high = float(scaling.get("low", 1.0)), float(scaling.get("high", 32.0))
-        if not low < high:
-            raise ValueError("scaling by parts needs low < high")
-        made = float(scaling["original"]) * f / (2 * math.pi)
+        original = float(scaling.get("original", 0.0))
+        if not low < high or not original > 0:
+            raise ValueError("scaling by parts needs low < high and the original length")
+        made = original * f / (2 * math.pi)
         keep = ((made - low) / (high - low)).clamp(0.0, 1.0)
         return f * keep + f / s * (1.0 - keep), 0.1 * math.log(s) + 1.0 if s > 1 else 1.0
 
@@ -728,7 +729,8 @@ class AdamW:
     all; CUDA, contiguous, bf16 / fp16 / fp32), one launch a step.
 
     ``grads``, of the same structure and shapes, in bf16, fp16 or fp32, are what a step reads; without them fp32 ones
-    are made, to be written by ``phi_backward(grads=opt.grads)``.  ``master=True`` keeps an fp32 copy of parameters that
+    are made, to be written by ``phi_backward(grads=opt.grads)``.  A step goes by the addresses that parameters and
+    gradients have here: assign into them (what replaces one in its dict, or its storage, is not seen).  ``master=True`` keeps an fp32 copy of parameters that
     are not fp32, which is what is updated (``reset_master`` after a change of the parameters from elsewhere).
     ``state_bits``: 32, or 8 for moments in 8 bits under an exponent for each 32 elements.
 
@@ -871,7 +873,8 @@ def distill_gradients(q, k, v, y, phi, grads, T, HW, chunk, overlap=0, rope_plan
     """Loss of one block's distillation (Eq. 19) on one batch, and the gradients of its feature maps, written to
     ``grads`` (a dict like ``phi``, fp32: an ``AdamW``'s): rotary positions (with a ``rope_plan``; q and k may then have
     any strides, see ``rope``), the forward pass, ``distill_loss`` against the teacher's output y, ``phi_backward`` on
-    that same forward pass.  Returns the loss, one fp32 on the device."""
+    that same forward pass.  The forward pass uses the library-held workspace: order such calls on one stream.  Returns
+    the loss, one fp32 on the device."""
     ctx = _elsewhere(q, stream) if q.is_cuda else None
     if ctx is not None:
         with ctx:
@@ -908,8 +911,9 @@ def distill_step(q, k, v, y, phi, opt, T, HW, chunk, lr=None, stream=None, **kw)
     launch, with AdamW([phi_0, phi_1, ...]), a ``distill_gradients`` into ``opt.grads[i]`` each, and ``opt.step()``.)
     Returns the loss before the update."""
     if not isinstance(opt.grads, dict) or opt.grads.keys() != phi.keys() or \
-            any(a is not b for a, b in zip(opt.params, phi.values())):
-        raise ValueError("opt must be an AdamW over this phi")
+            any(a is not b for a, b in zip(opt.params, phi.values())) or \
+            any(a is not b for a, b in zip(opt._grads, opt.grads.values())):
+        raise ValueError("opt must be an AdamW over this phi, and its grads those it was made with")
     ctx = _elsewhere(q, stream) if q.is_cuda else None
     if ctx is not None:
         with ctx:

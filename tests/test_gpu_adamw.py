@@ -275,20 +275,6 @@ def test_a_gradient_that_is_no_number():
             assert torch.equal(torch.isnan(m[:100].cpu()) | torch.isinf(v[:100].cpu()) | torch.isnan(v[:100].cpu()), lost)
 
 
-def test_8_bits_follow_32():
-    """A quadratic: both kinds of moments come as close to its lowest point as their last steps are long."""
-    target = torch.randn(5000, generator=torch.Generator().manual_seed(8)).cuda()
-    ends = []
-    for bits in (32, 8):
-        p = torch.zeros(5000, device="cuda")
-        opt = binding.AdamW([p], lr=0.02, weight_decay=0.0, state_bits=bits)
-        for i in range(300):
-            opt._grads[0].copy_(p - target)
-            opt.step()
-        ends.append((p - target).abs().mean().item())
-    assert max(ends) <= 0.02, ends
-
-
 # ---- how it is called -----------------------------------------------------------------------------------------------------
 
 
@@ -434,3 +420,38 @@ def test_feature_maps_of_a_block():
     grads, _ = binding.phi_backward(q, k, v, phi, G, T, HW, 1, grads=opt.grads)
     assert all(torch.equal(grads[n], want[n]) and grads[n] is opt.grads[n] for n in phi)
     check_step(opt)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_two_graphs_of_one_optimiser(bits):
+    """Steps at two rates, captured apart, replayed in turn: one state, one count."""
+    opt, pf, _ = make([5000, 33], BF16, FP32, bits, seed=20)
+    ref, rf, _ = make([5000, 33], BF16, FP32, bits, seed=20)
+    opt.step(), ref.step()
+    torch.cuda.synchronize()
+    graphs = []
+    for lr in (1e-3, 3e-3):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            opt.step(lr=lr)
+    for i in range(6):
+        graphs[i % 2].replay()
+        ref.step(lr=(1e-3, 3e-3)[i % 2])
+        torch.cuda.synchronize()
+        assert torch.equal(pf, rf) and int(opt.step_count.item()) == i + 2
+
+
+def test_two_optimisers_at_once():
+    sizes = [3000, 100000, 77]
+    pairs = [(make(sizes, BF16, FP32, bits, seed=21), make(sizes, BF16, FP32, bits, seed=21)) for bits in (32, 8)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in pairs]
+    for _ in range(10):
+        for s, (mine, _) in zip(streams, pairs):
+            mine[0].step(stream=s)
+        for _, ref in pairs:
+            ref[0].step()
+    torch.cuda.synchronize()
+    for mine, ref in pairs:
+        assert torch.equal(mine[1], ref[1]) and int(mine[0].step_count.item()) == 10
+        assert all(torch.equal(a, b) for a, b in zip(mine[0].moments(), ref[0].moments()))

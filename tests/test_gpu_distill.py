@@ -182,6 +182,11 @@ def test_refusals():
     with pytest.raises(ValueError):
         binding.distill_step(*args, phi, binding.AdamW([phi]), T, HW, 1)
     grads = opt.grads
+    mine = copy_phi(s["phi"])
+    moved = binding.AdamW(mine)
+    moved.grads["w1_q"] = moved.grads["w1_q"].clone()                # a gradient that the update would not read
+    with pytest.raises(ValueError):
+        binding.distill_step(*args, mine, moved, T, HW, 1, rope_plan=s["plan"], grid=s["grid"])
     with pytest.raises(TypeError):                                   # token-major without a rotation
         binding.distill_gradients(*args, phi, grads, T, HW, 1)
     with pytest.raises(ValueError):

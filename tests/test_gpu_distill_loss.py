@@ -201,3 +201,36 @@ def test_nothing_and_overlaps_are_refused():
             binding.distill_loss(y_hat, y, grad=grad)
         assert e.value.code == binding.E_SHAPE
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("weighted", [False, True])
+def test_offsets_beyond_32_bits(weighted):
+    """3 x 2^30 elements: the last ones stand 2^32 bytes and more behind the first."""
+    B, H, N, d = 1, 3, 2**24, 64
+    y_hat, y = (torch.zeros(B, H, N, d, device="cuda", dtype=BF16) for _ in range(2))
+    y_hat[0, 2, -1, 60:] = 3.0
+    y[0, 2, -2, 5] = 2.0
+    y_hat[0, 0, 0, 0] = -1.0
+    w = torch.full((B, N), 0.5, device="cuda") if weighted else None
+    loss, grad = binding.distill_loss(y_hat, y, scale=1.0, weight=w)
+    assert loss.item() == (15.0 if not weighted else 7.5)
+    one = 0.5 if weighted else 1.0
+    assert [int((grad[0, h] != 0).sum()) for h in range(H)] == [1, 0, 5]
+    assert grad[0, 0, 0, 0] == -one and grad[0, 2, -2, 5] == -one and (grad[0, 2, -1, 60:] == one).all()
+    del y_hat, y, grad
+    torch.cuda.empty_cache()
+
+
+def test_two_streams_at_once():
+    pairs = [tuple(t.cuda() for t in inputs(2, 3, 3000, 128, BF16, 20 + i)) for i in range(2)]
+    want = [binding.distill_loss(*p) for p in pairs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in pairs]
+    got = [[] for _ in pairs]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(10):
+        for s, p, g in zip(streams, pairs, got):
+            g.append(binding.distill_loss(*p, stream=s))
+    torch.cuda.synchronize()
+    assert all(torch.equal(l, w[0]) and torch.equal(x, w[1]) for g, w in zip(got, want) for l, x in g)

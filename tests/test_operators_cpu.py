@@ -5,6 +5,7 @@ import math
 import os
 import shutil
 import subprocess
+import types
 
 import pytest
 import torch
@@ -198,7 +199,8 @@ def test_turns_are_the_frequencies_modulo_a_turn():
 
 @pytest.mark.parametrize("bad", [
     dict(rot=3), dict(rot=0), dict(rot=130), dict(d=129, rot=128), dict(layout="other"), dict(sections=(32, 31)), dict(sections=(64, 0)),
-    dict(sections=(16, 16, 16, 16)), dict(scaling=dict(kind="no", factor=2.0)), dict(scaling=dict(kind="linear", factor=0.0)),
+    dict(sections=(16, 16, 16, 16)), dict(scaling=dict(kind="no", factor=2.0)), dict(scaling=dict(kind="linear")), dict(scaling=dict(factor=2.0)),
+    dict(scaling=dict(kind="parts", factor=2.0)), dict(scaling=dict(kind="base", factor=math.inf)), dict(scaling=dict(kind="linear", factor=0.0)),
     dict(scaling=dict(kind="parts", factor=2.0, original=100, low=2, high=2)), dict(freqs=[1.0]),
     dict(freqs=[1.0] * 64, scaling=dict(kind="linear", factor=2.0)),
 ])
@@ -362,3 +364,15 @@ def test_host_layers_under_asan_ubsan(tmp_path):
     assert r.returncode == 0, r.stdout + r.stderr
     assert "operators sanitize ok" in r.stdout
     assert "runtime error" not in r.stderr and "AddressSanitizer" not in r.stderr
+
+
+def test_work_belongs_to_the_tensors_device_and_stream(monkeypatch):
+    """Another current device is left for the tensors'; a stream of another device is refused."""
+    t = types.SimpleNamespace(device=torch.device("cuda:1"), get_device=lambda: 1)
+    monkeypatch.setattr(binding, "_current_device", lambda: 0)
+    ctx = binding._elsewhere(t, None)
+    assert isinstance(ctx, torch.cuda.device) and ctx.idx == 1
+    monkeypatch.setattr(binding, "_current_device", lambda: 1)
+    assert binding._elsewhere(t, None) is None
+    with pytest.raises(ValueError):
+        binding._elsewhere(t, types.SimpleNamespace(device=torch.device("cuda:0")))
