@@ -405,7 +405,8 @@ int rehyat_rope(const rehyat_rope_operand *operands, int n_operands,
  *   grad    same shape, bf16, overwritten: grad_out of rehyat_phi_backward.  NaN
  *           where y_hat or y is.
  *   loss    one fp32, DEVICE, overwritten
- * |y_hat - y| is formed in fp32 and summed in fp64 in a fixed order.
+ * w |y_hat - y| is formed in fp32, added up eight at a time in fp32 and those sums
+ * in fp64, in a fixed order.
  * y_hat, y and grad 16-byte aligned, weight and loss 4-byte; grad overlaps no input.
  * workspace: DEVICE, 256-byte aligned, rehyat_distill_loss_workspace_bytes(...)
  * bytes; nothing in it is assumed or survives.
@@ -445,8 +446,8 @@ int rehyat_distill_loss(const void *y_hat, const void *y, int type,
  *                       are c + 8 (v_exp - 30); 0 is 0.  Exponent 255: no element
  *                       of the group is a number any more (a gradient was not
  *                       finite, or a moment passed 2^127); bytes of v are 255 then.
- *                       The new moments are rounded once to fp32 (so from 1 - beta1
- *                       and 1 - beta2 in fp32), enter the update, and are rounded
+ *                       The new moments (with beta and 1 - beta as fp32 numbers)
+ *                       are rounded once to fp32, enter the update, and are rounded
  *                       from there to 8 bits, to nearest; a v that is not 0 never
  *                       becomes 0.
  * Pointers are aligned to their elements, m and v to 16 bytes.  Ranges that are
@@ -461,10 +462,11 @@ int rehyat_distill_loss(const void *y_hat, const void *y, int type,
  * with every replay.
  * rehyat_adamw_step: one update of all tensors.  lr_device (DEVICE fp32, nullable)
  * replaces lr, for schedules under replay.  Steps of one table must be ordered.
- * rehyat_adamw_moments: the values of n 8-bit moments, m and v in whole groups as above (DEVICE fp32 out,
- * 16-byte aligned).
+ * rehyat_adamw_moments: the values of n 8-bit moments, m and v in whole groups as
+ * above (DEVICE fp32 out, 16-byte aligned).
  * Errors: REHYAT_E_NULL, REHYAT_E_SHAPE (also: overlapping ranges; lr, eps or
- * weight_decay negative or not finite, eps below FLT_MIN, a beta outside [0, 1)), REHYAT_E_WORKSPACE.
+ * weight_decay negative or beyond fp32, eps below FLT_MIN, a beta outside [0, 1)),
+ * REHYAT_E_WORKSPACE.
  */
 typedef struct {
   void *param;

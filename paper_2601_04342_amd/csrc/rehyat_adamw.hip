@@ -386,7 +386,7 @@ bool apart(Range* r, size_t n) {
 }
 
 bool fraction(double x) { return x >= 0.0 && x < 1.0; }
-bool not_negative(double x) { return std::isfinite(x) && x >= 0.0; }
+bool not_negative(double x) { return x >= 0.0 && x <= FLT_MAX; }
 
 }  // namespace
 }  // namespace rehyat

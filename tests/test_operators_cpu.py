@@ -309,7 +309,8 @@ def test_adamw_prepare_rejects_sizes_and_tables():
 
 @pytest.mark.parametrize("bad", [
     dict(lr=-1.0), dict(lr=math.nan), dict(lr=math.inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.5),
-    dict(beta2=math.nan), dict(eps=0.0), dict(eps=-1.0), dict(eps=1e-60), dict(weight_decay=-0.1), dict(lr_device=A + 1),
+    dict(beta2=math.nan), dict(lr=1e39), dict(eps=1e39), dict(weight_decay=math.nan),
+    dict(eps=0.0), dict(eps=-1.0), dict(eps=1e-60), dict(weight_decay=-0.1), dict(lr_device=A + 1),
 ])
 def test_adamw_step_rejects(bad):
     plan = binding.AdamWPlan(A, 5, 2, 32)
