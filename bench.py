@@ -31,8 +31,8 @@ PEAK_BF16_TFLOPS = 2500.0   # MI355X dense bf16 MFMA, published
 # Anything else reports null.
 ATTN_TRAFFIC = {
     # 2.0 x 169,119 KiB + 1.0 x 98,280 KiB (profiles/wan480p_hbm_traffic_pmc.md), measured in version 308, whose
-    # forward kernels version 400 has unchanged
-    ("wan480p", "forward", 400): 447_000_000,
+    # forward kernels version 401 has unchanged
+    ("wan480p", "forward", 401): 447_000_000,
 }
 
 

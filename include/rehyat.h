@@ -446,10 +446,15 @@ int rehyat_distill_loss(const void *y_hat, const void *y, int type,
  *                       are c + 8 (v_exp - 30); 0 is 0.  Exponent 255: no element
  *                       of the group is a number any more (a gradient was not
  *                       finite, or a moment passed 2^127); bytes of v are 255 then.
- *                       The new moments (with beta and 1 - beta as fp32 numbers)
- *                       are rounded once to fp32, enter the update, and are rounded
- *                       from there to 8 bits, to nearest; a v that is not 0 never
- *                       becomes 0.
+ *                       The new moments enter the update in fp32 and are rounded
+ *                       from there to 8 bits; a v that is not 0 never becomes 0.
+ *                       Rounding goes up with the probability of how far the value
+ *                       is on its way from the code below to the one above, which
+ *                       keeps the moments' means, as rounding to nearest does not:
+ *                       what one update changes of v is less than half a step of
+ *                       its codes.  The random bits are a hash of the update's
+ *                       number and the element's place among all tensors in their
+ *                       order: the same for every run and replay.
  * Pointers are aligned to their elements, m and v to 16 bytes.  Ranges that are
  * written overlap no other range of any tensor.
  *
@@ -462,10 +467,16 @@ int rehyat_distill_loss(const void *y_hat, const void *y, int type,
  * with every replay.
  * rehyat_adamw_step: one update of all tensors.  lr_device (DEVICE fp32, nullable)
  * replaces lr, for schedules under replay.  Steps of one table must be ordered.
+ * nearest_steps (8-bit moments; not read with 32 bits): updates 1 .. nearest_steps
+ * round to nearest, from moments that are rounded to fp32 (with beta and 1 - beta as
+ * fp32 numbers) out of sums in fp64.  The first few updates change v by more than a
+ * step of its codes, and are then nearer; more than some ten of them lose what is
+ * said above, unless beta2 is so small that every update changes v by 1/8 of it.
  * rehyat_adamw_moments: the values of n 8-bit moments, m and v in whole groups as
  * above (DEVICE fp32 out, 16-byte aligned).
  * Errors: REHYAT_E_NULL, REHYAT_E_SHAPE (also: overlapping ranges; lr, eps or
- * weight_decay negative or beyond fp32, eps below FLT_MIN, a beta outside [0, 1)),
+ * weight_decay negative or beyond fp32, eps below FLT_MIN, a beta outside [0, 1),
+ * nearest_steps negative),
  * REHYAT_E_WORKSPACE.
  */
 typedef struct {
@@ -485,6 +496,7 @@ typedef struct {
 typedef struct {
   double lr, beta1, beta2, eps, weight_decay;
   const float *lr_device;
+  int64_t nearest_steps;
 } rehyat_adamw_hyper;
 size_t rehyat_adamw_table_bytes(const int64_t *sizes, int n_tensors);
 int rehyat_adamw_prepare(const rehyat_adamw_tensor *tensors, int n_tensors,

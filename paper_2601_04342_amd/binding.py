@@ -87,7 +87,7 @@ class AdamWPlan(ctypes.Structure):
 
 class AdamWHyper(ctypes.Structure):
     _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [
-        ("lr_device", ctypes.c_void_p)]
+        ("lr_device", ctypes.c_void_p), ("nearest_steps", ctypes.c_int64)]
 
 
 class RehyatError(RuntimeError):
@@ -732,16 +732,20 @@ class AdamW:
     are made, to be written by ``phi_backward(grads=opt.grads)``.  A step goes by the addresses that parameters and
     gradients have here: assign into them (what replaces one in its dict, or its storage, is not seen).  ``master=True`` keeps an fp32 copy of parameters that
     are not fp32, which is what is updated (``reset_master`` after a change of the parameters from elsewhere).
-    ``state_bits``: 32, or 8 for moments in 8 bits under an exponent for each 32 elements.
+    ``state_bits``: 32, or 8 for moments in 8 bits under an exponent for each 32 elements.  Those are rounded at random,
+    by bits that depend on the step and the element alone, so that they follow the means of g and g^2; steps up to number
+    ``nearest_steps``, which change them by more than their rounding does, to nearest (with many of those, and the usual
+    betas, v stays far behind: see the header).
 
-    ``lr``, ``betas``, ``eps`` and ``weight_decay`` may be set between steps.  State: ``m``, ``v`` (fp32, or e4m3 and
+    ``lr``, ``betas``, ``eps``, ``weight_decay`` and ``nearest_steps`` may be set between steps.  State: ``m``, ``v`` (fp32, or e4m3 and
     uint8 with ``m_exp``, ``v_exp``), each one buffer in which tensor i begins at ``offsets[i]``; ``master``, likewise at
     ``master_offsets[i]`` (None: no copy); ``step_count``, on the device."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, master=True,
-                 grads=None):
+                 grads=None, nearest_steps=8):
         self.params = _leaves(params)
         self.lr, self.betas, self.eps, self.weight_decay, self.state_bits = lr, betas, eps, weight_decay, state_bits
+        self.nearest_steps = nearest_steps
         if not self.params:
             raise ValueError("no parameters")
         if state_bits not in (8, 32):
@@ -820,7 +824,7 @@ class AdamW:
             if lr.dtype != torch.float32 or lr.numel() != 1 or lr.device != self.m.device:
                 raise TypeError("lr must be a number or one fp32 on the parameters' device")
             lr, at = 0.0, lr.data_ptr()
-        method = (lr, *self.betas, self.eps, self.weight_decay, at)
+        method = (lr, *self.betas, self.eps, self.weight_decay, at, self.nearest_steps)
         if method != self._method:   # the struct as it is otherwise: 1.2 of 6 us
             self._hyper, self._method = AdamWHyper(*method), method
         rc = self._step(ctypes.byref(self._plan), ctypes.byref(self._hyper), _stream_handle(None))

@@ -9,9 +9,16 @@
 // Moments in 8 bits: groups of 32 elements share an exponent, a power of two, so scaling is exact and every rounding is
 // one of the format's own.  m is e4m3 (what the card converts to and from in hardware); v has no sign and needs range
 // more than m does: 5 bits of exponent, 3 of mantissa, no zero exponent, which is the leading 11 bits of an fp32
-// number less a constant of the group, so that both directions are a few integer instructions.  Rounded to nearest it
-// keeps 1/16 of v, 1/32 of the square root that divides the update.  v that is not 0 keeps a code of at least 1: a
-// divisor that fell to 0 beside an m that did not would make the update unbounded.
+// number less a constant of the group, so that both directions are a few integer instructions.  v that is not 0 keeps a
+// code of at least 1: a divisor that fell to 0 beside an m that did not would make the update unbounded.
+//
+// A step of these formats is 1/8 to 1/16 of the value, an update changes v by 1/1000 of it at beta2 = 0.999: rounded to
+// nearest, nearly every change would be lost, and v would neither follow the mean of g^2 up (a quarter of it after 3,000
+// updates with normal gradients) nor fall when gradients do (13 times it, 5,000 updates after they fell to a tenth).  So
+// codes are rounded at random, up with the probability that leaves the mean where it was: v is then right in the mean and
+// off by 0.2 of itself, which makes the update's rms 1.03 of what it is with 32 bits.  The random bits are a hash of the
+// update's number and the element's place, so runs and replays agree.  The first updates change v by more than a step, and
+// are rounded to nearest (hyper.nearest_steps).
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
@@ -116,16 +123,50 @@ __device__ __forceinline__ f32x4 decode_v(uint32_t codes, int e) {
   }
   return x;
 }
+// one code of v, of an fp32 number's bits and what is added to them before those beyond the code are cut off
+__device__ __forceinline__ uint32_t code_v(uint32_t bits, uint32_t more, int e) {
+  int c = (int)((bits + more) >> 20) - ((e - 30) << 3);
+  c = c < 1 ? 1 : c > 255 ? 255 : c;
+  return bits == 0 ? 0u : (uint32_t)c;
+}
 __device__ __forceinline__ uint32_t encode_v(f32x4 v, int e) {
   uint32_t codes = 0;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const uint32_t bits = bits_of(v[k]);
-    int c = (int)((bits + 0x7ffffu + ((bits >> 20) & 1)) >> 20) - ((e - 30) << 3);
-    c = c < 1 ? 1 : c > 255 ? 255 : c;
-    codes |= (bits == 0 ? 0u : (uint32_t)c) << (8 * k);
+    codes |= code_v(bits, 0x7ffffu + ((bits >> 20) & 1), e) << (8 * k);
   }
   return e == 255 ? ~0u : codes;
+}
+
+// 32 bits of x's that differ in any way: two rounds of folding the upper half down and multiplying, with the fractions of
+// the roots of 2 and 3 as odd factors.
+__host__ __device__ __forceinline__ uint32_t scatter(uint32_t x) {
+  x ^= x >> 16;
+  x *= 0x6a09e667u;
+  x ^= x >> 15;
+  x *= 0xbb67ae85u;
+  return x ^ x >> 16;
+}
+// Codes rounded up with a probability of how far the value is on its way there: 20 random bits are added to the 20 that the
+// code does not keep of v, and 16 (with half of the last) to those that it does not keep of m.  An element's two share the
+// four bits that count least for v.  e4m3's smallest numbers have no exponent of their own: below 2^-6 the value in
+// steps of 2^-9, with 20 bits behind them, is what stands for the bits above.
+// (element k's hash is that of place + k, exclusive or `mix`)
+__device__ __forceinline__ void encode_random(f32x4 m, f32x4 v, int em, int ev, uint32_t place, uint32_t mix, uint32_t* cm,
+                                              uint32_t* cv) {
+  const float f = power_of_two(261 - em);
+  uint32_t x = 0, y = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t random = scatter((place + k) ^ mix);
+    const float a = __builtin_fabsf(m[k]) * f;   // up to 256
+    const uint32_t bits = a < 0x1p-6f ? (uint32_t)(a * 0x1p29f) : bits_of(a) - (120u << 23);
+    x |= (((bits + ((random & 0xffff) << 4 | 8)) >> 20) | (bits_of(m[k]) >> 24 & 0x80)) << (8 * k);
+    y |= code_v(bits_of(v[k]), random >> 12, ev) << (8 * k);
+  }
+  *cm = em == 255 ? 0u : x;
+  *cv = ev == 255 ? ~0u : y;
 }
 // largest over the eight lanes that hold a group: neighbours, pairs, then the two halves mirrored
 __device__ __forceinline__ uint32_t group_max(uint32_t x) {
@@ -204,7 +245,7 @@ struct StepArgs {
   double exact[4];                         // the first four in 64 bits
   float keep;                              // 1 - lr weight_decay
   int32_t n_tensors, counters;
-  int64_t items;
+  int64_t items, nearest_steps;
 };
 
 // Root and, in the step, reciprocal are the hardware's approximations, off by one in the last place: the update keeps 21
@@ -288,6 +329,7 @@ __global__ __launch_bounds__(kThreads, BITS == 32 ? kWaves32 : kWaves8) void ada
 
   // factors of this update, and the workgroup's arrival (its answer is not looked at before the end)
   __shared__ float factors[3];
+  __shared__ uint32_t rounding[2];   // whether to nearest; otherwise what the update's number adds to the hash
   int64_t step = 0;
   uint32_t before = 0;
   const uint32_t counters = a.counters, mine = blockIdx.x % counters;
@@ -297,15 +339,23 @@ __global__ __launch_bounds__(kThreads, BITS == 32 ? kWaves32 : kWaves8) void ada
     const float c = -expm1f((float)((double)step * (threadIdx.x ? a.log_beta2 : a.log_beta1)));
     factors[threadIdx.x] = threadIdx.x ? 1.f / sqrtf(c) : lr / c;
     factors[2] = a.lr_device ? (float)(1.0 - (double)lr * a.weight_decay) : a.keep;
+    rounding[0] = step <= a.nearest_steps;
+    rounding[1] = scatter((uint32_t)step * 0x9e3779b9u + (uint32_t)(step >> 32));   // the golden ratio's fraction
   }
   __syncthreads();
   if (threadIdx.x == 0)
     before = __hip_atomic_fetch_add(&header->counter[mine].arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  const float rate = factors[0], root = factors[1], keep = factors[2];
+  // (in scalar registers: there are just as many others as six waves may have)
+  auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+  auto factor = [&](int k) { return __builtin_bit_cast(float, scalar(bits_of(factors[k]))); };
+  const float rate = factor(0), root = factor(1), keep = factor(2);
+  const bool nearest = scalar(rounding[0]);
+  const uint32_t key = scalar(rounding[1]);
 
   for (int64_t item = blockIdx.x; item < a.items; ) {
     const Piece e = c;
     const Quad<BITS> y = x;
+    const int64_t place = item * kItem;   // of the item's first element among all
     item += gridDim.x;
     if (item < a.items) fetch(item);   // in flight behind what follows
     if (!active(e)) continue;
@@ -319,21 +369,33 @@ __global__ __launch_bounds__(kThreads, BITS == 32 ? kWaves32 : kWaves8) void ada
     } else {
       m = decode_m(y.cm, y.em);
       v = decode_v(y.cv, y.ev);
-      // in 64 bits, where products of 24-bit numbers are exact: m, v are the true sums rounded once, so that what
-      // lies half way between two codes is decided by the numbers and not by how they were added
+      if (nearest) {
+        // in 64 bits, where products of 24-bit numbers are exact: sums rounded once there and once to fp32, so that what
+        // lies half way between two codes is decided by the numbers and not by how they were added
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const double g = y.g[k];
+          m[k] = (float)fma(a.exact[0], (double)m[k], a.exact[1] * g);
+          v[k] = (float)fma(a.exact[2], (double)v[k], a.exact[3] * (g * g));
+        }
+      } else {
+        m = a.beta1 * m + a.rest1 * y.g;
+        v = a.beta2 * v + a.rest2 * (y.g * y.g);
+      }
       uint32_t top_m = 0, top_v = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const double g = y.g[k];
-        m[k] = (float)fma(a.exact[0], (double)m[k], a.exact[1] * g);
-        v[k] = (float)fma(a.exact[2], (double)v[k], a.exact[3] * (g * g));
         const uint32_t bm = bits_of(m[k]) & 0x7fffffffu, bv = bits_of(v[k]) & 0x7fffffffu;
         top_m = bm > top_m ? bm : top_m;
         top_v = bv > top_v ? bv : top_v;
       }
       const int em = group_exponent(group_max(top_m), kLeastM), ev = group_exponent(group_max(top_v), kLeastV);
-      *at<uint32_t>(e.m, i / 4) = encode_m(m, em);
-      *at<uint32_t>(e.v, i / 4) = encode_v(v, ev);
+      uint32_t cm, cv;
+      if (nearest) cm = encode_m(m, em), cv = encode_v(v, ev);
+      else   // (places from 2^32 on change the key)
+        encode_random(m, v, em, ev, (uint32_t)place + i, key + (uint32_t)(place >> 32) * 0x9e3779b9u, &cm, &cv);
+      *at<uint32_t>(e.m, i / 4) = cm;
+      *at<uint32_t>(e.v, i / 4) = cv;
       if (threadIdx.x % (kGroup / 4) == 0) {
         *at<uint8_t>(e.m_exp, i / kGroup) = em;
         *at<uint8_t>(e.v_exp, i / kGroup) = ev;
@@ -482,7 +544,7 @@ int rehyat_adamw_step(const rehyat_adamw_plan* plan, const rehyat_adamw_hyper* h
   if (plan->items < 1 || plan->n_tensors < 1 || (plan->state_bits != 32 && plan->state_bits != 8)) return REHYAT_E_SHAPE;
   if (!aligned(plan->table, 256)) return REHYAT_E_WORKSPACE;
   if (!not_negative(hyper->lr) || !not_negative(hyper->weight_decay) || !not_negative(hyper->eps) ||
-      !((float)hyper->eps >= FLT_MIN) || !fraction(hyper->beta1) || !fraction(hyper->beta2))
+      !((float)hyper->eps >= FLT_MIN) || !fraction(hyper->beta1) || !fraction(hyper->beta2) || hyper->nearest_steps < 0)
     return REHYAT_E_SHAPE;
   if (hyper->lr_device && !aligned4(hyper->lr_device)) return REHYAT_E_SHAPE;
   StepArgs a;
@@ -504,6 +566,7 @@ int rehyat_adamw_step(const rehyat_adamw_plan* plan, const rehyat_adamw_hyper* h
   a.keep = (float)(1.0 - hyper->lr * hyper->weight_decay);
   a.n_tensors = plan->n_tensors;
   a.items = plan->items;
+  a.nearest_steps = hyper->nearest_steps;
   const int waves = plan->state_bits == 32 ? kWaves32 : kWaves8, lds = (160 * 1024 / waves - 64) & ~1023;
   const int grid = (int)std::min<int64_t>(plan->items, 256 * waves);
   a.counters = 1;   // as many as arrive at each

@@ -754,7 +754,7 @@ int rehyat::hip_fail(hipError_t e, const char* what) {
 
 extern "C" {
 
-int rehyat_version(void) { return 400; }
+int rehyat_version(void) { return 401; }
 
 const char* rehyat_status_string(int code) {
   switch (code) {
