@@ -249,6 +249,7 @@ def prepare(case, seed):
         st["opt"] = binding.AdamW(params, lr=_LR, betas=(_B1, _B2), eps=_EPS, weight_decay=_WD, state_bits=c["bits"],
                                   master=c["master"], grads=[grad[o:o + k] for o, k in at])
         st["opt"].load_state(st["m"], st["v"], _STEP, m_exp=st.get("me"), v_exp=st.get("ve"))
+        st["opt"].nearest_steps = 1 << 62   # codes as the plain form rounds them; by default this update's are rounded at random
         if c["bits"] == 8:
             st["values"] = [torch.empty(n, device="cuda") for _ in range(2)]
     return st
