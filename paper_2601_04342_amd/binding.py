@@ -708,6 +708,17 @@ def _leaves(x):
     return [t for v in (x.values() if isinstance(x, dict) else x) for t in _leaves(v)]
 
 
+def _leaves_like(x, y):
+    """The tensors of ``y`` in the order of those of ``x``, which has its structure: dicts go by their keys."""
+    if isinstance(x, torch.Tensor) != isinstance(y, torch.Tensor) or isinstance(x, dict) != isinstance(y, dict) or \
+            not isinstance(x, torch.Tensor) and (x.keys() != y.keys() if isinstance(x, dict) else len(x) != len(y)):
+        raise ValueError("grads must have a tensor for each parameter, in the same structure")
+    if isinstance(x, torch.Tensor):
+        return [y]
+    pairs = ((v, y[n]) for n, v in x.items()) if isinstance(x, dict) else zip(x, y)
+    return [t for a, b in pairs for t in _leaves_like(a, b)]
+
+
 def _like(x, tensors):
     """The structure of ``x`` with the tensors of an iterator in it."""
     if isinstance(x, torch.Tensor):
@@ -728,7 +739,7 @@ class AdamW:
     """AdamW over all of ``params`` (tensors in nested dicts and lists: the phi of one block, or a list of the phi of
     all; CUDA, contiguous, bf16 / fp16 / fp32), one launch a step.
 
-    ``grads``, of the same structure and shapes, in bf16, fp16 or fp32, are what a step reads; without them fp32 ones
+    ``grads``, of the same structure (dicts by their keys) and shapes, in bf16, fp16 or fp32, are what a step reads; without them fp32 ones
     are made, to be written by ``phi_backward(grads=opt.grads)``.  A step goes by the addresses that parameters and
     gradients have here: assign into them (what replaces one in its dict, or its storage, is not seen).  ``master=True`` keeps an fp32 copy of parameters that
     are not fp32, which is what is updated (``reset_master`` after a change of the parameters from elsewhere).
@@ -744,6 +755,7 @@ class AdamW:
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, master=True,
                  grads=None, nearest_steps=8):
         self.params = _leaves(params)
+        self._names = list(params) if isinstance(params, dict) else None
         self.lr, self.betas, self.eps, self.weight_decay, self.state_bits = lr, betas, eps, weight_decay, state_bits
         self.nearest_steps = nearest_steps
         if not self.params:
@@ -767,9 +779,7 @@ class AdamW:
             self._grads = [flat[o:o + n].view(p.shape) for o, n, p in zip(self.offsets, sizes, self.params)]
             self.grads = _like(params, iter(self._grads))
         else:
-            self._grads, self.grads = _leaves(grads), grads
-            if len(self._grads) != len(self.params):
-                raise ValueError("grads must have a tensor for each parameter")
+            self._grads, self.grads = _leaves_like(params, grads), grads
             for p, g in zip(self.params, self._grads):
                 if g.dtype not in _TYPES or g.device != dev or not g.is_contiguous() or g.shape != p.shape:
                     raise TypeError("grads must be contiguous CUDA tensors shaped like the parameters")
@@ -914,9 +924,10 @@ def distill_step(q, k, v, y, phi, opt, T, HW, chunk, lr=None, stream=None, **kw)
     phi <- AdamW(phi).  ``opt`` is an ``AdamW`` over ``phi``, a dict.  (Several blocks share one optimiser, and one
     launch, with AdamW([phi_0, phi_1, ...]), a ``distill_gradients`` into ``opt.grads[i]`` each, and ``opt.step()``.)
     Returns the loss before the update."""
-    if not isinstance(opt.grads, dict) or opt.grads.keys() != phi.keys() or \
-            any(a is not b for a, b in zip(opt.params, phi.values())) or \
-            any(a is not b for a, b in zip(opt._grads, opt.grads.values())):
+    names = opt._names
+    if names is None or set(names) != phi.keys() or opt.grads.keys() != phi.keys() or \
+            any(a is not phi[n] for n, a in zip(names, opt.params)) or \
+            any(a is not opt.grads[n] for n, a in zip(names, opt._grads)):
         raise ValueError("opt must be an AdamW over this phi, and its grads those it was made with")
     ctx = _elsewhere(q, stream) if q.is_cuda else None
     if ctx is not None:

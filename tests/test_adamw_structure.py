@@ -1,0 +1,58 @@
+"""Which gradient belongs to which parameter of an AdamW, and what a state that is loaded replaces."""
+import pytest
+import torch
+
+from paper_2601_04342_amd import binding, synth
+
+
+def test_gradients_are_found_by_their_keys():
+    t = [torch.zeros(1) for _ in range(8)]
+    params = {"a": t[0], "b": [t[1], {"x": t[2], "y": t[3]}]}
+    grads = {"b": (t[5], {"y": t[7], "x": t[6]}), "a": t[4]}
+    got = binding._leaves_like(params, grads)
+    assert len(got) == 4 and all(a is b for a, b in zip(got, t[4:]))
+    for bad in ({"a": t[4]}, {"a": t[4], "b": (t[5],)}, {"a": t[4], "c": grads["b"]}, [t[4], grads["b"]], t[4],
+                {"a": [t[4]], "b": grads["b"]}, {"a": t[4], "b": (t[5], t[6])}, {**grads, "c": t[7]}):
+        with pytest.raises(ValueError):
+            binding._leaves_like(params, bad)
+
+
+def turned(x):
+    """The same dict with queries' and keys' entries in each other's places, which fit in shape."""
+    return {m: x[m] for m in (n[:-1] + {"q": "k", "k": "q"}[n[-1]] for n in x)}
+
+
+@pytest.mark.gpu
+def test_a_dict_of_gradients_in_another_order():
+    start = binding.phi_to_device(synth.make_phi(2, 64, seed=1))
+    want, phi = ({n: t.clone() for n, t in start.items()} for _ in range(2))
+    ref = binding.AdamW(want)
+    grads = {n: torch.randn(t.shape, generator=torch.Generator().manual_seed(i)).cuda() for i, (n, t) in enumerate(phi.items())}
+    for n, g in grads.items():
+        ref.grads[n].copy_(g)
+    opt = binding.AdamW(phi, grads=turned(grads))
+    opt.step(), ref.step()
+    assert all(torch.equal(phi[n], want[n]) and not torch.equal(phi[n], start[n]) for n in start)
+    with pytest.raises(ValueError):
+        binding.AdamW(phi, grads={n: g for n, g in grads.items() if n != "b2_k"})
+
+
+@pytest.mark.gpu
+def test_a_step_of_distillation_goes_by_names():
+    B, H, T, HW, d = 1, 2, 4, 60, 64
+    q, k, v = (t.to("cuda", torch.bfloat16) for t in synth.make_qkv(B, H, T * HW, d, seed=2))
+    start = binding.phi_to_device(synth.make_phi(H, d, seed=3, gain=4.0))
+    y = binding.forward(q, k, v, start, T, HW, T)
+    want, phi = ({n: t.clone() for n, t in start.items()} for _ in range(2))
+    ref = binding.AdamW(want)
+    opt = binding.AdamW(phi, grads=turned({n: torch.zeros(t.shape, device="cuda") for n, t in phi.items()}))
+    for _ in range(2):
+        a = binding.distill_step(q, k, v, y, want, ref, T, HW, 1)
+        b = binding.distill_step(q, k, v, y, turned(phi), opt, T, HW, 1)
+        assert torch.equal(a, b) and all(torch.equal(phi[n], want[n]) for n in phi)
+    swapped = {**phi, "w1_q": phi["w1_k"], "w1_k": phi["w1_q"]}
+    with pytest.raises(ValueError):
+        binding.distill_step(q, k, v, y, swapped, opt, T, HW, 1)
+    opt.grads["w1_q"], opt.grads["w1_k"] = opt.grads["w1_k"], opt.grads["w1_q"]
+    with pytest.raises(ValueError):
+        binding.distill_step(q, k, v, y, phi, opt, T, HW, 1)
