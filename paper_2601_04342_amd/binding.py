@@ -864,7 +864,8 @@ class AdamW:
         return m, v
 
     def load_state(self, m, v, step, m_exp=None, v_exp=None, master=None):
-        """Copies a state in (buffers as in ``m``, ``v``, ``m_exp``, ``v_exp``, ``master``; ``step`` updates made)."""
+        """Copies a state in (buffers as in ``m``, ``v``, ``m_exp``, ``v_exp``, ``master``; ``step`` updates made).  Without
+        a ``master`` the fp32 copies are made of the parameters as they are now."""
         step = int(step)
         if step < 0:
             raise ValueError("step must not be negative")
@@ -879,6 +880,8 @@ class AdamW:
         for mine, other in given:
             if mine is not None:
                 mine.copy_(other)
+        if master is None:
+            self.reset_master()
         self.step_count.fill_(step)
 
 

@@ -56,3 +56,20 @@ def test_a_step_of_distillation_goes_by_names():
     opt.grads["w1_q"], opt.grads["w1_k"] = opt.grads["w1_k"], opt.grads["w1_q"]
     with pytest.raises(ValueError):
         binding.distill_step(q, k, v, y, phi, opt, T, HW, 1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_state_without_fp32_copies(bits):
+    """A checkpoint's weights are copied into the parameters, its moments loaded: the next step starts from those weights."""
+    g = torch.Generator().manual_seed(4)
+    weights = (torch.randn(700, generator=g) * 0.02).to("cuda", torch.bfloat16)
+    grad = torch.randn(700, generator=g).cuda() * 1e-3
+    fresh = binding.AdamW([weights.clone()], state_bits=bits)
+    resumed = binding.AdamW([torch.zeros_like(weights)], state_bits=bits)
+    resumed.params[0].copy_(weights)
+    resumed.load_state(fresh.m, fresh.v, 0, m_exp=fresh.m_exp, v_exp=fresh.v_exp)
+    for o in (fresh, resumed):
+        o._grads[0].copy_(grad)
+        o.step()
+    assert torch.equal(fresh.master, resumed.master) and torch.equal(fresh.params[0], resumed.params[0])
