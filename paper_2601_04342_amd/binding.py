@@ -867,8 +867,8 @@ class AdamW:
         """Copies a state in (buffers as in ``m``, ``v``, ``m_exp``, ``v_exp``, ``master``; ``step`` updates made).  Without
         a ``master`` the fp32 copies are made of the parameters as they are now."""
         step = int(step)
-        if step < 0:
-            raise ValueError("step must not be negative")
+        if not 0 <= step < 2**63:
+            raise ValueError("step must not be negative, and fit 64 bits")
         given = [(self.m, m), (self.v, v), (self.m_exp, m_exp), (self.v_exp, v_exp)]
         if master is not None:
             given.append((self.master, master))

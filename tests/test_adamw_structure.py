@@ -73,3 +73,15 @@ def test_a_state_without_fp32_copies(bits):
         o._grads[0].copy_(grad)
         o.step()
     assert torch.equal(fresh.master, resumed.master) and torch.equal(fresh.params[0], resumed.params[0])
+
+
+def test_a_step_that_is_no_count_is_refused_before_anything_is_copied():
+    opt = binding.AdamW.__new__(binding.AdamW)      # its buffers on the host
+    opt.m, opt.v, opt.m_exp, opt.v_exp, opt.master = torch.zeros(4), torch.zeros(4), None, None, None
+    opt.params, opt.master_offsets, opt.step_count = [], [], torch.zeros((), dtype=torch.int64)
+    for bad in (-1, 2**63):
+        with pytest.raises(ValueError):
+            opt.load_state(torch.ones(4), torch.ones(4), bad)
+        assert (opt.m == 0).all() and (opt.v == 0).all()
+    opt.load_state(torch.ones(4), torch.ones(4), 2**63 - 1)
+    assert (opt.m == 1).all() and opt.step_count.item() == 2**63 - 1
