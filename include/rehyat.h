@@ -473,7 +473,7 @@ int rehyat_distill_loss(const void *y_hat, const void *y, int type,
  * step of its codes, and are then nearer; more than some ten of them lose what is
  * said above, unless beta2 is so small that every update changes v by 1/8 of it.
  * rehyat_adamw_moments: the values of n 8-bit moments, m and v in whole groups as
- * above (DEVICE fp32 out, 16-byte aligned).
+ * above (DEVICE fp32 out, 16-byte aligned), n < 2^38.
  * Errors: REHYAT_E_NULL, REHYAT_E_SHAPE (also: overlapping ranges; lr, eps or
  * weight_decay negative or beyond fp32, eps below FLT_MIN, a beta outside [0, 1),
  * nearest_steps negative),

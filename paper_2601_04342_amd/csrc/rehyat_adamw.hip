@@ -593,10 +593,15 @@ int rehyat_adamw_moments(const void* m, const void* m_exp, const void* v, const 
                     {(uintptr_t)m_out, (uintptr_t)m_out + 4 * n, true}, {(uintptr_t)v_out, (uintptr_t)v_out + 4 * n, true}};
   if (!apart(ranges, 6)) return REHYAT_E_SHAPE;
   auto* const kernel = past_caches(10 * n) ? adamw_moments_kernel<true> : adamw_moments_kernel<false>;
-  kernel<<<(unsigned)((n + 4 * kThreads - 1) / (4 * kThreads)), kThreads, 0, (hipStream_t)stream>>>(
-      (const uint8_t*)m, (const uint8_t*)m_exp, (const uint8_t*)v, (const uint8_t*)v_exp, m_out, v_out, n);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return hip_fail(e, "AdamW moments kernel launch");
+  // threads of a launch are counted in 32 bits: 2^31 of them at most, four elements each
+  for (int64_t lo = 0, most = (int64_t)1 << 33; lo < n; lo += most) {
+    const int64_t count = std::min(n - lo, most);
+    kernel<<<(unsigned)((count + kItem - 1) / kItem), kThreads, 0, (hipStream_t)stream>>>(
+        (const uint8_t*)m + lo, (const uint8_t*)m_exp + lo / kGroup, (const uint8_t*)v + lo,
+        (const uint8_t*)v_exp + lo / kGroup, m_out + lo, v_out + lo, count);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return hip_fail(e, "AdamW moments kernel launch");
+  }
   return REHYAT_OK;
 }
 
