@@ -11,13 +11,15 @@ from paper_2601_04342_amd import binding, build
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
-def recorder(tmp_path_factory, name):
+@pytest.fixture(scope="module")
+def record(tmp_path_factory):
+    """run("moments" | "positions" | "loss", ...) -> (status, grids) of a call whose launches are recorded, not made."""
     if shutil.which("gcc") is None:
         pytest.skip("gcc not available")
     binding.library()
-    exe = str(tmp_path_factory.mktemp("host") / name)
-    subprocess.run(["gcc", "-O1", "-rdynamic", os.path.join(ROOT, "tests", "host", name + ".c"), "-o", exe, "-ldl"], check=True,
-                   capture_output=True, text=True)
+    exe = str(tmp_path_factory.mktemp("host") / "record_places")
+    subprocess.run(["gcc", "-O1", "-rdynamic", os.path.join(ROOT, "tests", "host", "record_places.c"), "-o", exe, "-ldl"],
+                   check=True, capture_output=True, text=True)
 
     def run(*args):
         r = subprocess.run([exe, build.LIB, *map(str, args)], capture_output=True, text=True, timeout=120, check=True)
@@ -27,19 +29,14 @@ def recorder(tmp_path_factory, name):
     return run
 
 
-@pytest.fixture(scope="module")
-def record_moments(tmp_path_factory):
-    return recorder(tmp_path_factory, "record_moments")
-
-
 @pytest.mark.parametrize("n", [1, 1024, 1025, 10**6, 2**33, 2**33 + 1, 2**34 - 1, 2**34 + 5, 2**38 - 1])
-def test_moments_of_any_size_fit_the_runtimes_grids(record_moments, n):
+def test_moments_of_any_size_fit_the_runtimes_grids(record, n):
     """A grid's threads are counted in 32 bits."""
-    status, launches = record_moments("-", n)
+    status, launches = record("moments", n)
     assert status == binding.OK
     assert all(0 < int(x) * 256 < 2**32 and y == z == "1" for x, y, z in launches)
     assert sum(int(x) for x, _, _ in launches) == -(-n // 1024)
 
 
-def test_moments_beyond_what_is_supported(record_moments):
-    assert record_moments("-", 2**38) == (binding.E_SHAPE, [])
+def test_moments_beyond_what_is_supported(record):
+    assert record("moments", 2**38) == (binding.E_SHAPE, [])
