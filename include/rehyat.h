@@ -348,7 +348,9 @@ int rehyat_step(const void *q_t, const void *k_win, const void *v_win,
  *             n / cols % rows, n % cols), by the number of axes.
  *             Otherwise DEVICE integers of `bits` (32 or 64): position x of token
  *             n of sequence b at data[b stride_b + n stride_n + x]
- *             (stride_b 0: the same for all); negative ones are allowed.
+ *             (stride_b 0: the same for all); negative ones are allowed.  They lie
+ *             outside of the range from the first to the last element of each out,
+ *             as `turns` must.
  * rehyat_rope_operand (HOST struct): a tensor of `heads` rows of d elements for
  *   each of B x N tokens.  Strides in elements (>= 0; those of x may be 0), rows
  *   themselves contiguous, pointers aligned to an element: token-major projections

@@ -316,6 +316,9 @@ int rehyat_rope(const rehyat_rope_operand* operands, int n_operands, const rehya
       for (int64_t v : {in[i].stride[k], out[i].stride[k]})
         if (v < 0 || v > ((int64_t)1 << 46) / in[i].extent[k]) return REHYAT_E_SHAPE;   // sums of products fit 64 bits
     if (!span_of(out[i], d)) return REHYAT_E_SHAPE;
+    if (a.pos && !ranges_apart(o.out, span_of(out[i], d) * (int64_t)es, a.pos,
+                               ((B - 1) * a.pos_b + (N - 1) * a.pos_n + axes) * (a.pos_bits / 8)))
+      return REHYAT_E_SHAPE;
     a.op[i] = {o.x, o.out, o.x_stride_b, o.x_stride_h, o.x_stride_n, o.out_stride_b, o.out_stride_h, o.out_stride_n, o.heads};
   }
   for (int i = 0; i < n_operands; ++i)

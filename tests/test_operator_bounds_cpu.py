@@ -40,3 +40,20 @@ def test_moments_of_any_size_fit_the_runtimes_grids(record, n):
 
 def test_moments_beyond_what_is_supported(record):
     assert record("moments", 2**38) == (binding.E_SHAPE, [])
+
+
+OUT, SECOND, OUT_BYTES = 1 << 40, 2 << 40, 2 * 3 * 8 * 64 * 2      # B = 2, 3 heads, N = 8, 64 elements of two bytes
+
+
+@pytest.mark.parametrize("bits,axes,strides,size", [
+    (32, 1, (0, 1), 32), (64, 1, (8, 1), 128), (32, 3, (24, 3), 192), (64, 2, (0, 2), 128), (32, 1, (100, 4), 4 * (100 + 28 + 1)),
+    (64, 1, (0, 0), 8),
+])
+@pytest.mark.parametrize("out", [OUT, SECOND])
+def test_rope_positions_are_not_written_over(record, bits, axes, strides, size, out):
+    """A workgroup would read what another has turned already."""
+    word = bits // 8
+    for at, taken in ((out + OUT_BYTES, True), (out + OUT_BYTES - word, False), (out - size, True), (out - size + word, False),
+                      (out + 2048, False)):
+        status, launches = record("positions", bits, axes, 2, 8, *strides, at, OUT, SECOND)
+        assert (status, len(launches)) == ((binding.OK, 1) if taken else (binding.E_SHAPE, 0)), at - out
