@@ -409,7 +409,9 @@ int rehyat_rope(const rehyat_rope_operand *operands, int n_operands,
  *   loss    one fp32, DEVICE, overwritten
  * w |y_hat - y| is formed in fp32, added up eight at a time in fp32 and those sums
  * in fp64, in a fixed order.
- * y_hat, y and grad 16-byte aligned, weight and loss 4-byte; grad overlaps no input.
+ * y_hat, y and grad 16-byte aligned, weight and loss 4-byte; grad overlaps no input, loss
+ * and workspace overlap neither y_hat, y nor grad (which is checked), and weight is
+ * outside of the workspace (which is not).
  * workspace: DEVICE, 256-byte aligned, rehyat_distill_loss_workspace_bytes(...)
  * bytes; nothing in it is assumed or survives.
  * Supported: B * H <= 65535, N * d < 2^31.

@@ -199,8 +199,14 @@ int rehyat_distill_loss(const void* y_hat, const void* y, int type, const float*
   if (!ranges_apart(grad, 2 * n, y_hat, 2 * n) || !ranges_apart(grad, 2 * n, y, n * (int64_t)type_bytes(type)) ||
       (weight && !ranges_apart(grad, 2 * n, weight, (int64_t)4 * B * N)))
     return REHYAT_E_SHAPE;
-  if (!aligned(workspace, 256) || workspace_bytes < rehyat_distill_loss_workspace_bytes(B, H, N, d))
-    return REHYAT_E_WORKSPACE;
+  const size_t need = rehyat_distill_loss_workspace_bytes(B, H, N, d);
+  if (!aligned(workspace, 256) || workspace_bytes < need) return REHYAT_E_WORKSPACE;
+  const struct {
+    const void* at;
+    int64_t bytes;
+  } used[] = {{y_hat, 2 * n}, {grad, 2 * n}, {y, n * (int64_t)type_bytes(type)}};
+  for (const auto& u : used)
+    if (!ranges_apart(loss, 4, u.at, u.bytes) || !ranges_apart(workspace, (int64_t)need, u.at, u.bytes)) return REHYAT_E_SHAPE;
   LossArgs a;
   a.y_hat = (const uint16_t*)y_hat;
   a.y = y;

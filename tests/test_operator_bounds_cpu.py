@@ -57,3 +57,29 @@ def test_rope_positions_are_not_written_over(record, bits, axes, strides, size, 
                       (out + 2048, False)):
         status, launches = record("positions", bits, axes, 2, 8, *strides, at, OUT, SECOND)
         assert (status, len(launches)) == ((binding.OK, 1) if taken else (binding.E_SHAPE, 0)), at - out
+
+
+GB = 1 << 30
+LARGE, SMALL = (2, 3, 4001, 64), (1, 2, 100, 64)                   # two launches, one launch
+
+
+@pytest.mark.parametrize("B,H,N,d", [LARGE, SMALL])
+@pytest.mark.parametrize("type_", [0, 2])
+def test_loss_and_workspace_overlap_nothing_that_is_read_or_written(record, B, H, N, d, type_):
+    n = B * H * N * d
+    room = binding.distill_loss_workspace_bytes(B, H, N, d)
+    far = dict(y_hat=GB, y=2 * GB, weight=0, grad=3 * GB, loss=4 * GB, workspace=5 * GB)
+    run = lambda **at: record("loss", type_, B, H, N, d, *{**far, **at}.values())
+    launches = 1 if (B, H, N, d) == SMALL else 2
+    assert run() == (binding.OK, run()[1]) and len(run()[1]) == launches
+    assert len(run(weight=6 * GB)[1]) == launches
+    for name, size in (("y_hat", 2 * n), ("y", (4 if type_ == 2 else 2) * n), ("grad", 2 * n)):
+        for at in (far[name], far[name] + size - 4, far[name] + size // 2 // 4 * 4):
+            assert run(loss=at) == (binding.E_SHAPE, []), (name, at)
+        last = far[name] + (size - 1) // 256 * 256
+        for at in (far[name], last, far[name] - room + 256):
+            assert run(workspace=at) == (binding.E_SHAPE, []), (name, at)
+        assert run(loss=far[name] + size)[0] == run(loss=far[name] - 4)[0] == binding.OK
+        assert run(workspace=far[name] - room)[0] == run(workspace=last + 256)[0] == binding.OK
+    # the sum of the pieces' sums is written when all of them have been read
+    assert run(loss=far["workspace"])[0] == binding.OK
