@@ -24,8 +24,9 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 # are fenced slot by slot, so it moves only what stands around them.  In the other files it made those calls 1.4 %
 # slower (the chunk-state kernel) and gradients 0.6 % faster: they keep the default
 EXTRA_FLAGS = {"rehyat_attn.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"],
-               # NaN in the inputs is told from numbers there
-               "rehyat_loss.hip": ["-fhonor-nans"], "rehyat_adamw.hip": ["-fhonor-nans"]}
+               # NaN in the inputs is told from numbers, or stays in its pair, there
+               "rehyat_rope.hip": ["-fhonor-nans"], "rehyat_loss.hip": ["-fhonor-nans"],
+               "rehyat_adamw.hip": ["-fhonor-nans"]}
 
 
 def build_library(force=True, verbose=False):

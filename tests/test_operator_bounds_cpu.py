@@ -83,3 +83,11 @@ def test_loss_and_workspace_overlap_nothing_that_is_read_or_written(record, B, H
         assert run(workspace=far[name] - room)[0] == run(workspace=last + 256)[0] == binding.OK
     # the sum of the pieces' sums is written when all of them have been read
     assert run(loss=far["workspace"])[0] == binding.OK
+
+
+@pytest.mark.parametrize("source", ["rehyat_rope.hip", "rehyat_loss.hip", "rehyat_adamw.hip"])
+def test_sources_that_meet_numbers_that_are_none_are_compiled_for_them(source):
+    """What such an element becomes is stated and tested: nothing of it may be taken to be impossible."""
+    flags = [f for f in build.FLAGS + build.EXTRA_FLAGS.get(source, []) if f.endswith("honor-nans")]
+    assert flags[-1] == "-fhonor-nans"
+    assert not [f for f in build.FLAGS if "fast-math" in f or "finite" in f or f == "-fno-honor-infinities"]
