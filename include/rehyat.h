@@ -329,8 +329,8 @@ int rehyat_step(const void *q_t, const void *k_win, const void *v_win,
  *
  * Angles are formed in fixed point: a frequency is held as the 2^-64 parts of a
  * turn that a step of one position makes (rehyat_rope_turns), so the product
- * with a position, modulo 2^64, is the angle modulo a turn, however far the
- * position.  cos, sin and the rotation are evaluated in fp32; results are
+ * with a position, modulo 2^64, is the angle modulo a turn, without a reduction
+ * that would lose more the farther the position.  cos, sin and the rotation are evaluated in fp32; results are
  * rounded once.
  *
  * rehyat_rope_plan (HOST struct)
@@ -388,7 +388,8 @@ typedef struct {
   int64_t out_stride_b, out_stride_h, out_stride_n;
   int32_t heads;
 } rehyat_rope_operand;
-/* HOST: radians a position (any finite value) -> 2^-64 parts of a turn. */
+/* HOST: radians a position (any finite value) -> 2^-64 parts of a turn, off by at
+ * most half of one, and by 2^-63 of the number of turns. */
 int rehyat_rope_turns(const double *radians, int n, uint64_t *turns);
 int rehyat_rope(const rehyat_rope_operand *operands, int n_operands,
                 const rehyat_rope_plan *plan,

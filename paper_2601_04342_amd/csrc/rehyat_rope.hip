@@ -2,8 +2,9 @@
 //
 // Pair i of a head row turns by angle = position * frequency.  Frequencies come as 2^-64 parts of a turn a position, so
 // the 64-bit product, which wraps, IS the angle modulo a turn; its upper 32 bits (2^-32 of a turn is 1.5e-9 rad) give the
-// quadrant and an angle within an eighth of a turn, where short series for cos and sin serve.  No far position loses more
-// than a near one.
+// quadrant and an angle within an eighth of a turn, where short series for cos and sin serve.  No reduction adds to what a
+// far position makes of the frequency's own rounding: position times 2^-64 turns at most, which 2^32 positions take to that
+// cut-off (what a double is off by is some hundred times as much, at one radian a position).
 //
 // Bound by HBM: each element is read and written once, and needs 3 flops.  A thread keeps the cos and sin of its one or
 // two pairs and walks over the heads of its token with them, since they are the same for every head, four heads in
@@ -50,7 +51,7 @@ struct RopeArgs {
 };
 
 // cos and sin of an angle given in 2^-32 turns: within an eighth of a turn of the nearest quarter, the series in the
-// angle (the first term left out is below 2e-9 of the result), then the quarter turns.
+// angle (the first term left out is 2.5e-9 of the result at most), then the quarter turns.
 __device__ __forceinline__ void cos_sin(uint32_t t, float* c, float* s) {
   const uint32_t quarter = (t + 0x20000000u) >> 30;
   const float x = (float)(int32_t)(t - (quarter << 30)) * 1.46291807926715968e-9f;   // 2 pi 2^-32
@@ -257,8 +258,8 @@ int rehyat_rope_turns(const double* radians, int n, uint64_t* turns) {
   for (int i = 0; i < n; ++i) {
     long double t = (long double)radians[i] / 6.28318530717958647692528676655900577L;
     t -= std::floor(t);                       // in [0, 1]: 1 where a tiny negative one rounds up
-    t = std::ldexp(t, 64);
-    turns[i] = t >= 18446744073709551615.0L ? 0 : (uint64_t)t;
+    t = std::rint(std::ldexp(t, 64));
+    turns[i] = t >= 18446744073709551616.0L ? 0 : (uint64_t)t;
   }
   return REHYAT_OK;
 }

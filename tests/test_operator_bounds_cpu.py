@@ -1,8 +1,11 @@
 """Sizes and places at which calls of the operators around the attention are refused, or are cut into launches that the
 runtime takes: without a GPU, the pointers are fake."""
+import ctypes
 import os
+import random
 import shutil
 import subprocess
+from fractions import Fraction
 
 import pytest
 
@@ -91,3 +94,24 @@ def test_sources_that_meet_numbers_that_are_none_are_compiled_for_them(source):
     flags = [f for f in build.FLAGS + build.EXTRA_FLAGS.get(source, []) if f.endswith("honor-nans")]
     assert flags[-1] == "-fhonor-nans"
     assert not [f for f in build.FLAGS if "fast-math" in f or "finite" in f or f == "-fno-honor-infinities"]
+
+
+# 1 / (2 pi) to 120 places, from a series for pi in whole numbers: pi = 16 atan(1/5) - 4 atan(1/239)
+def _turns_of(radians):
+    one = 10**140
+    atan = lambda k: sum((-1)**i * (one // k**(2 * i + 1)) // (2 * i + 1) for i in range(110))
+    pi = Fraction(16 * atan(5) - 4 * atan(239), one)
+    return Fraction(radians) / (2 * pi) * 2**64
+
+
+@pytest.mark.parametrize("scale", [1e-6, 1e-3, 1.0, 100.0, 1e6])
+def test_turns_are_rounded_to_the_nearest(scale):
+    """Half a unit, and what the quotient in 64 bits is off by: its own rounding and that of 2 pi, each 2^-64 of it."""
+    rng = random.Random(int(scale * 1e6))
+    f = [rng.choice((-1, 1)) * scale * rng.uniform(0.1, 1) for _ in range(64)]
+    t = (ctypes.c_uint64 * 64)()
+    assert binding.library().rehyat_rope_turns((ctypes.c_double * 64)(*f), 64, t) == binding.OK
+    for x, got in zip(f, t):
+        want = _turns_of(x)
+        off = (got - want) % 2**64
+        assert min(off, 2**64 - off) <= Fraction(1, 2) + abs(want) / 2**63 + Fraction(1, 10**6), x
