@@ -403,7 +403,8 @@ int rehyat_rope(const rehyat_rope_operand *operands, int n_operands,
  *   y       same shape, of `type`: the teacher's
  *   weight  [B, N] fp32 DEVICE, nullable (1): a factor for each token.  Where it
  *           is 0, G is 0 and the elements do not count, whatever they hold (the
- *           padding of a batch).
+ *           padding of a batch).  rehyat_phi_backward multiplies that G with y_hat
+ *           and with feature maps of q: for it they must be finite there.
  *   scale   1 / (number of elements that count) gives the mean of Eq. 19
  *   grad    same shape, bf16, overwritten: grad_out of rehyat_phi_backward.  NaN
  *           where y_hat or y is.

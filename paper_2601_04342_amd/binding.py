@@ -890,8 +890,9 @@ def distill_gradients(q, k, v, y, phi, grads, T, HW, chunk, overlap=0, rope_plan
     """Loss of one block's distillation (Eq. 19) on one batch, and the gradients of its feature maps, written to
     ``grads`` (a dict like ``phi``, fp32: an ``AdamW``'s): rotary positions (with a ``rope_plan``; q and k may then have
     any strides, see ``rope``), the forward pass, ``distill_loss`` against the teacher's output y, ``phi_backward`` on
-    that same forward pass.  The forward pass uses the library-held workspace: order such calls on one stream.  Returns
-    the loss, one fp32 on the device."""
+    that same forward pass.  Tokens of ``weight`` 0 do not count, but their q, k and v must be finite: they go through
+    the forward pass, and its gradient multiplies what comes of them by 0.  (Their y may hold anything.)  The forward pass
+    uses the library-held workspace: order such calls on one stream.  Returns the loss, one fp32 on the device."""
     ctx = _elsewhere(q, stream) if q.is_cuda else None
     if ctx is not None:
         with ctx:
