@@ -34,10 +34,15 @@ constexpr int kThreads = 256;
 constexpr int kItem = 4 * kThreads;    // elements of an item: four a thread
 constexpr int kGroup = 32;
 
-// Workgroups of a step say that they have read `step`, each to one of kCounters counters in a cache line of its own, and
-// the last of each to `arrived`: atomics on one address are done one after the other, 45 ns each, and the step of one
-// block's eight tensors (71 MB, 2,048 workgroups) took 97 us with all of them on one counter, at its end; now 14 us.
-constexpr int kCounters = 64;
+// Workgroups a CU holds at most (see adamw_kernel), of 256 CUs.
+constexpr int kWaves32 = 4, kWaves8 = 6;
+
+// Workgroups of a step say that they have read `step`, each to one of up to kCounters counters in a cache line of its own,
+// as many as arrive at each, and the last of each to `arrived`: atomics on one address are done one after the other, 45 ns
+// each, and the step of one block's eight tensors (71 MB) took 97 us with all of 2,048 workgroups on one counter, at its
+// end; now, of 1,024 on 32, 14 us.
+constexpr int kCounters = 40;
+static_assert(kCounters * kCounters >= 256 * kWaves32 && kCounters * kCounters >= 256 * kWaves8, "for the largest grid");
 struct Header {
   int64_t step;      // updates made (the caller may see and set it)
   uint32_t arrived;  // counters that are full
@@ -293,12 +298,11 @@ struct Quad {
   int em, ev;
 };
 
-// Workgroups a CU holds, which is also waves a SIMD: one round of them walks over all items.  Shared memory that nobody
+// Workgroups a CU holds (kWaves32, kWaves8), which is also waves a SIMD: one round of them walks over all items.  Shared memory that nobody
 // uses keeps further ones out, so that no CU gets more of the round than another.  Of 3 / 4 / 5 / 6 the 200 tensors of 25
 // blocks take 400 / 316 / 319 / 324 us (more of them open more rows of memory than it holds); 8-bit moments, with more
 // arithmetic to hide, 473 / 316 / 303 / 299 (all but the first before their codes went through the caches, with which
 // it is 278).
-constexpr int kWaves32 = 4, kWaves8 = 6;
 template <int BITS, bool NT>
 __global__ __launch_bounds__(kThreads, BITS == 32 ? kWaves32 : kWaves8) void adamw_kernel(StepArgs a) {
   Header* const header = (Header*)a.table;
@@ -570,7 +574,7 @@ int rehyat_adamw_step(const rehyat_adamw_plan* plan, const rehyat_adamw_hyper* h
   const int waves = plan->state_bits == 32 ? kWaves32 : kWaves8, lds = (160 * 1024 / waves - 64) & ~1023;
   const int grid = (int)std::min<int64_t>(plan->items, 256 * waves);
   a.counters = 1;   // as many as arrive at each
-  while (a.counters * a.counters < grid && a.counters < kCounters) ++a.counters;
+  while (a.counters * a.counters < grid) ++a.counters;
   // past the caches 1,778 MB take 316 us against 338, through them 71 MB 14.1 against 15.2; codes of 8-bit moments, half a
   // line to a wave's instruction, always go through them (278 us against 299)
   const bool nt = past_caches(plan->items * kItem * (plan->state_bits == 32 ? 30 : 18));
