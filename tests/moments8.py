@@ -62,9 +62,12 @@ def _scatter(x):
 
 
 def random_bits(step, places):
-    """The hash of an update's number and of elements' places (each tensor begins at a multiple of 1,024)."""
+    """The hash of an update's number and of the places of four elements each (a tensor begins at a multiple of 1,024
+    elements), of which each element has the bits from another byte on."""
     step, golden, mask = int(step), 0x9E3779B9, 0xFFFFFFFF
-    places = np.asarray(places, np.uint64)
+    places, left = np.divmod(np.asarray(places, np.uint64), np.uint64(4))
+    left *= np.uint64(8)
     key = int(_scatter(np.array([(step * golden + (step >> 32)) & mask], np.uint64))[0])
     mix = (np.uint64(key) + (places >> np.uint64(32)) * np.uint64(golden)) & np.uint64(mask)
-    return _scatter((places & np.uint64(mask)) ^ mix)
+    h = _scatter((places & np.uint64(mask)) ^ mix)
+    return ((h << left) | (h >> (np.uint64(32) - left))) & np.uint64(mask)

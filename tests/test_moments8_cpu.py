@@ -79,7 +79,7 @@ def test_random_bits_are_spread():
     for part in (lambda x: (x & np.uint64(0xFFFF)) / 2**16, lambda x: (x >> np.uint64(12)) / 2**20):
         x = part(steps)
         assert abs(x.mean() - 0.5) <= 0.0102 and abs(np.corrcoef(x[:-1], x[1:])[0, 1]) <= 0.036
-    far = moments8.random_bits(9, np.arange(64, dtype=np.uint64) + np.uint64(2**32))
+    far = moments8.random_bits(9, np.arange(64, dtype=np.uint64) + np.uint64(2**34))
     assert (far != moments8.random_bits(9, np.arange(64))).sum() > 60
 
 
