@@ -427,7 +427,7 @@ template <bool NT>
 __global__ __launch_bounds__(kThreads) void adamw_moments_kernel(const uint8_t* m, const uint8_t* m_exp, const uint8_t* v,
                                                                  const uint8_t* v_exp, float* m_out, float* v_out,
                                                                  int64_t n) {
-  const int64_t i = 4 * ((int64_t)blockIdx.x * kThreads + threadIdx.x);
+  const uint32_t i = 4 * (blockIdx.x * kThreads + threadIdx.x);   // n is 2^32 at most
   if (i >= n) return;
   const int left = n - i < 4 ? (int)(n - i) : 4;
   store4<NT, Fp32, f32x4>(m_out, i, left, decode_m(*(const uint32_t*)(m + i), m_exp[i / kGroup]));
@@ -599,8 +599,8 @@ int rehyat_adamw_moments(const void* m, const void* m_exp, const void* v, const 
                     {(uintptr_t)m_out, (uintptr_t)m_out + 4 * n, true}, {(uintptr_t)v_out, (uintptr_t)v_out + 4 * n, true}};
   if (!apart(ranges, 6)) return REHYAT_E_SHAPE;
   auto* const kernel = past_caches(10 * n) ? adamw_moments_kernel<true> : adamw_moments_kernel<false>;
-  // threads of a launch are counted in 32 bits: 2^31 of them at most, four elements each
-  for (int64_t lo = 0, most = (int64_t)1 << 33; lo < n; lo += most) {
+  // elements of a launch, as its threads, are counted in 32 bits
+  for (int64_t lo = 0, most = (int64_t)1 << 32; lo < n; lo += most) {
     const int64_t count = std::min(n - lo, most);
     kernel<<<(unsigned)((count + kItem - 1) / kItem), kThreads, 0, (hipStream_t)stream>>>(
         (const uint8_t*)m + lo, (const uint8_t*)m_exp + lo / kGroup, (const uint8_t*)v + lo,

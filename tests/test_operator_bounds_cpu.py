@@ -34,10 +34,10 @@ def record(tmp_path_factory):
 
 @pytest.mark.parametrize("n", [1, 1024, 1025, 10**6, 2**33, 2**33 + 1, 2**34 - 1, 2**34 + 5, 2**38 - 1])
 def test_moments_of_any_size_fit_the_runtimes_grids(record, n):
-    """A grid's threads are counted in 32 bits."""
+    """A grid's threads, and the elements of a launch, are counted in 32 bits."""
     status, launches = record("moments", n)
     assert status == binding.OK
-    assert all(0 < int(x) * 256 < 2**32 and y == z == "1" for x, y, z in launches)
+    assert all(0 < int(x) * 256 < 2**32 and int(x) * 1024 <= 2**32 and y == z == "1" for x, y, z in launches)
     assert sum(int(x) for x, _, _ in launches) == -(-n // 1024)
 
 
