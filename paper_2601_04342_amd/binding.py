@@ -795,11 +795,12 @@ class AdamW:
         self.master = zeros(total, torch.float32) if total else None
         self.reset_master()
 
+    @torch.no_grad()   # parameters may be leaves of an autograd graph, of which the copies are no part
     def reset_master(self):
         """The fp32 copies <- the parameters as they are now."""
-        for p, o in zip(self.params, self.master_offsets):
-            if o is not None:
-                self.master[o:o + p.numel()].copy_(p.view(-1))
+        held = [(self.master[o:o + p.numel()].view(p.shape), p) for p, o in zip(self.params, self.master_offsets) if o is not None]
+        if held:
+            torch._foreach_copy_(*zip(*held))   # 100 tensors: 100 us, with a call for each 590
 
     def _prepare(self, step):
         n = len(self.params)
@@ -863,6 +864,7 @@ class AdamW:
             raise RehyatError(rc, "rehyat_adamw_moments")
         return m, v
 
+    @torch.no_grad()
     def load_state(self, m, v, step, m_exp=None, v_exp=None, master=None):
         """Copies a state in (buffers as in ``m``, ``v``, ``m_exp``, ``v_exp``, ``master``; ``step`` updates made).  Without
         a ``master`` the fp32 copies are made of the parameters as they are now."""

@@ -85,3 +85,22 @@ def test_a_step_that_is_no_count_is_refused_before_anything_is_copied():
         assert (opt.m == 0).all() and (opt.v == 0).all()
     opt.load_state(torch.ones(4), torch.ones(4), 2**63 - 1)
     assert (opt.m == 1).all() and opt.step_count.item() == 2**63 - 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_copies_of_leaves_are_no_part_of_their_graphs(dtype):
+    g = torch.Generator().manual_seed(5)
+    start = [(torch.randn(3, 70, generator=g) * 0.02).to("cuda", dtype), torch.ones((), device="cuda", dtype=dtype),
+             torch.randn(5, generator=g).cuda(), torch.zeros(0, 4, device="cuda", dtype=dtype)]
+    opt = binding.AdamW([torch.nn.Parameter(t.clone()) for t in start])
+    plain = binding.AdamW([t.clone() for t in start])
+    for o in (opt, plain):
+        for i, t in enumerate(o._grads):
+            t.fill_(1e-3 * (i + 1))
+        o.step()
+        o.reset_master()
+        o.load_state(o.m.clone(), o.v.clone(), 1)
+        o.step()
+        assert not any(t.requires_grad for t in (o.master, o.m, o.v))
+    assert torch.equal(opt.master, plain.master) and all(torch.equal(a, b) for a, b in zip(opt.params, plain.params))
