@@ -453,14 +453,17 @@ int rehyat_distill_loss(const void *y_hat, const void *y, int type,
  *                       of the group is a number any more (a gradient was not
  *                       finite, or a moment passed 2^127); bytes of v are 255 then.
  *                       The new moments enter the update in fp32 and are rounded
- *                       from there to 8 bits; a v that is not 0 never becomes 0.
+ *                       from there to 8 bits; a v that is not 0 never becomes 0
+ *                       (nor less than 2^-31 of its group's largest: elements with
+ *                       gradients below 2^-15 of the group's move less).
  *                       Rounding goes up with the probability of how far the value
  *                       is on its way from the code below to the one above, which
  *                       keeps the moments' means, as rounding to nearest does not:
  *                       what one update changes of v is less than half a step of
  *                       its codes.  The random bits are a hash of the update's
- *                       number and the element's place among all tensors in their
- *                       order: the same for every run and replay.
+ *                       number and the element's place, where tensors in their order
+ *                       begin at multiples of 1,024: the same for every run and
+ *                       replay.
  * Pointers are aligned to their elements, m and v to 16 bytes.  Ranges that are
  * written overlap no other range of any tensor.
  *

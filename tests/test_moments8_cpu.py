@@ -87,3 +87,25 @@ def test_a_negative_count_of_nearest_steps_is_refused():
     plan = binding.AdamWPlan(0x1000, 5, 2, 8)
     h = binding.AdamWHyper(1e-3, 0.9, 0.999, 1e-8, 0.01, None, -1)
     assert binding.library().rehyat_adamw_step(ctypes.byref(plan), ctypes.byref(h), None) == binding.E_SHAPE
+
+
+def test_gradients_of_many_sizes_in_a_group():
+    """Down to 2^-15 of the largest (v spans 30 binades) updates are AdamW's; below that v is held up by its least code and they
+    shrink.  No m that is rounded up from next to nothing, to 2^-17 of the largest, meets a smaller divisor than 2^-15."""
+    n, (b1, b2), rng = 1024, (0.9, 0.999), np.random.default_rng(1)
+    spread = 2.0**-(np.arange(n) % 32)
+    codes = moments8.encode(np.zeros(n, F), np.zeros(n, F))
+    M, V, squares = np.zeros(n), np.zeros(n), np.zeros((2, 32))
+    for t in range(1, 1001):
+        g = (rng.normal(size=n) * 1e-3 * spread).astype(F)
+        m, v = moments8.decode(*codes)
+        m, v = F(b1) * m.astype(F) + F(1 - b1) * g, F(b2) * v.astype(F) + F(1 - b2) * (g * g)
+        M, V = b1 * M + (1 - b1) * g.astype(float), b2 * V + (1 - b2) * g.astype(float)**2
+        codes = moments8.encode(m, v, moments8.random_bits(t, np.arange(n)) if t > 8 else None)
+        mine, exact = (a / (1 - b1**t) / np.sqrt(b / (1 - b2**t)) for a, b in ((m, v), (M, V)))
+        # (after 8 updates to the nearest: an update of 1 is the first one's, 7.3 the most that AdamW makes of any gradients)
+        assert np.abs(mine).max() <= 1.25 * max(1.0, np.abs(exact).max()), t
+        if t > 500:
+            squares += [(x * x).reshape(-1, 32).mean(0) for x in (mine, exact)]
+    rms = np.sqrt(squares[0] / squares[1])
+    assert (np.abs(rms[:15] - 1) <= RMS).all() and (rms[15:] <= 1 + RMS).all()
