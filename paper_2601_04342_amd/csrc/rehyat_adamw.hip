@@ -4,7 +4,7 @@
 // element stand against 18 (moments in 8 bits) to 30 bytes.  A table in device memory, written when the tensors are
 // named, cuts all of them into items of 1,024 elements, so that one launch serves any number of tensors of any size
 // without the host touching them again.  The eight tensors of one block (71 MB, half in the caches) take 14.1 us, those of
-// 25 blocks (1,778 MB) 315 us, 5.6 TB/s; with 8-bit moments (1,075 MB) 195 us, 5.5 TB/s, and 83 us to read those back.
+// 25 blocks (1,778 MB) 302 us, 5.9 TB/s; with 8-bit moments (1,075 MB) 186 us, 5.8 TB/s, and 83 us to read those back.
 //
 // Moments in 8 bits: groups of 32 elements share an exponent, a power of two, so scaling is exact and every rounding is
 // one of the format's own.  m is e4m3 (what the card converts to and from in hardware); v has no sign and needs range
@@ -254,7 +254,7 @@ struct StepArgs {
 
 // Root and, in the step, reciprocal are the hardware's approximations, off by one in the last place: the update keeps 21
 // bits and more, and with exact ones, 18 instructions an element more, a step of 25 blocks with 8-bit moments took 11 us
-// longer, of 245.  The root's argument is scaled out of the denormals, which the instruction takes for 0; divisors are
+// longer, of 245, and with 32 bits a step of one block 0.6 us longer, of 12.7.  The root's argument is scaled out of the denormals, which the instruction takes for 0; divisors are
 // normal numbers, since eps is.
 __device__ __forceinline__ float root_of(float v) {
   const bool small = v < 0x1p-96f;
