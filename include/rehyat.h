@@ -330,8 +330,8 @@ int rehyat_step(const void *q_t, const void *k_win, const void *v_win,
  * Angles are formed in fixed point: a frequency is held as the 2^-64 parts of a
  * turn that a step of one position makes (rehyat_rope_turns), so the product
  * with a position, modulo 2^64, is the angle modulo a turn, without a reduction
- * that would lose more the farther the position.  cos, sin and the rotation are evaluated in fp32; results are
- * rounded once.
+ * that would lose more the farther the position.  cos, sin and the rotation are
+ * evaluated in fp32; results are rounded once.
  *
  * rehyat_rope_plan (HOST struct)
  *   turns     DEVICE, rot / 2 values of rehyat_rope_turns

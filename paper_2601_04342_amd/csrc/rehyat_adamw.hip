@@ -146,7 +146,7 @@ __device__ __forceinline__ uint32_t encode_v(f32x4 v, int e) {
 
 // 32 bits of x's that differ in any way: two rounds of folding the upper half down and multiplying, with the fractions of
 // the roots of 2 and 3 as odd factors.
-__host__ __device__ __forceinline__ uint32_t scatter(uint32_t x) {
+__device__ __forceinline__ uint32_t scatter(uint32_t x) {
   x ^= x >> 16;
   x *= 0x6a09e667u;
   x ^= x >> 15;
@@ -254,8 +254,8 @@ struct StepArgs {
 
 // Root and, in the step, reciprocal are the hardware's approximations, off by one in the last place: the update keeps 21
 // bits and more, and with exact ones, 18 instructions an element more, a step of 25 blocks with 8-bit moments took 11 us
-// longer, of 245, and with 32 bits a step of one block 0.6 us longer, of 12.7.  The root's argument is scaled out of the denormals, which the instruction takes for 0; divisors are
-// normal numbers, since eps is.
+// longer, of 245, and with 32 bits a step of one block 0.6 us longer, of 12.7.  The root's argument is scaled out of the
+// denormals, which the instruction takes for 0; divisors are normal numbers, since eps is.
 __device__ __forceinline__ float root_of(float v) {
   const bool small = v < 0x1p-96f;
   return __builtin_amdgcn_sqrtf(small ? v * 0x1p32f : v) * (small ? 0x1p-16f : 1.f);
@@ -297,11 +297,11 @@ struct Quad {
   int em, ev;
 };
 
-// Workgroups a CU holds (kWaves32, kWaves8), which is also waves a SIMD: one round of them walks over all items.  Shared memory that nobody
-// uses keeps further ones out, so that no CU gets more of the round than another.  Of 3 / 4 / 5 / 6 the 200 tensors of 25
-// blocks take 400 / 316 / 319 / 324 us (more of them open more rows of memory than it holds); 8-bit moments, with more
-// arithmetic to hide, 473 / 316 / 303 / 299 (all but the first before their codes went through the caches, with which
-// it is 278).
+// Workgroups a CU holds (kWaves32, kWaves8), which is also waves a SIMD: one round of them walks over all items.  Shared
+// memory that nobody uses keeps further ones out, so that no CU gets more of the round than another.  Of 3 / 4 / 5 / 6 the
+// 200 tensors of 25 blocks take 400 / 316 / 319 / 324 us (more of them open more rows of memory than it holds); 8-bit
+// moments, with more arithmetic to hide, 473 / 316 / 303 / 299, their values' reading included (before their codes went
+// through the caches, with which 6 take 278).
 template <int BITS, bool NT>
 __global__ __launch_bounds__(kThreads, BITS == 32 ? kWaves32 : kWaves8) void adamw_kernel(StepArgs a) {
   Header* const header = (Header*)a.table;
