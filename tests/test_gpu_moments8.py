@@ -115,3 +115,37 @@ def test_steps_to_the_nearest_are_checked_and_may_be_set():
     with pytest.raises(binding.RehyatError) as e:
         opts[0].step()
     assert e.value.code == binding.E_SHAPE
+
+
+def test_replays_and_moved_states_are_rounded_alike():
+    """The random bits go by the count on the device: a captured step rounds every replay by its own number, as eager steps
+    and those of an optimiser that took over the state do."""
+    def fresh():
+        g = torch.Generator().manual_seed(9)
+        opt = binding.AdamW([torch.zeros(k, device="cuda") for k in (5000, 33)], state_bits=8, nearest_steps=1)
+        for t in opt._grads:
+            t.copy_(torch.randn(t.shape, generator=g) * 1e-3)
+        opt.step()
+        return opt
+
+    opt, ref, other = fresh(), fresh(), fresh()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step()
+    codes = []
+    for i in range(6):
+        graph.replay()
+        torch.cuda.synchronize()
+        ref.step()
+        if i == 3:
+            other.load_state(ref.m, ref.v, ref.step_count, m_exp=ref.m_exp, v_exp=ref.v_exp)
+            for a, b in zip(other.params, ref.params):
+                a.copy_(b)
+        elif i > 3:
+            other.step()
+        for o in (ref,) if i < 3 else (ref, other):
+            assert torch.equal(opt.v, o.v) and torch.equal(opt.m.view(torch.uint8), o.m.view(torch.uint8)), i
+            assert all(torch.equal(a, b) for a, b in zip(opt.params, o.params)), i
+        codes.append(opt.v.clone())
+    assert not any(torch.equal(a, b) for a, b in zip(codes, codes[1:]))
